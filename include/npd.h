@@ -405,6 +405,71 @@ int npd_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, i
                   const void* B, int64_t ldb, int32_t b_mn_major, void* out, int64_t ldo,
                   int32_t out_mode, int32_t k_splits, void* cuda_stream);
 
+/* flags of npd_norm_args */
+enum { NPD_NORM_POST = 1 /* the branch goes through a norm of its own before it is added */ };
+
+/*
+ * The join of a block's branch with the residual stream, fused with the norms on both sides of it
+ * (root-mean-square norms): what a block's output passes through on its way to the next block, or
+ * to the LM head of npd_kd_fwd_bwd / npd_ce_fwd_bwd.
+ *
+ *   n[t,c] = x[t,c] r_x[t] (post_weight[c] + weight_offset)      with NPD_NORM_POST, else n = x
+ *   h[t,c] = residual_scale * residual[t,c] + branch_scale * gate[t,c] * n[t,c]
+ *   y[t,c] = h[t,c] r_h[t] (pre_weight[c] + weight_offset)
+ *   r_v[t] = 1 / sqrt(mean_c v[t,c]^2 + eps)
+ *
+ * A missing residual counts as 0, a missing x as no branch, a missing gate as 1; a NULL gain is 1
+ * (weight_offset does not apply to it).  With h = NULL only y is written (a plain norm: x or residual
+ * alone, y), with y = NULL only the join.  Rows are independent of each other.
+ *
+ * x, gate, y and their gradients are bf16; residual, h and their gradients are of `stream_dtype`; the
+ * gains are of `weight_dtype`, their gradients fp32.  All arithmetic is fp32 and each result is rounded once;
+ * y is taken from the unrounded h.  Layouts are row-major with row strides in ELEMENTS; every matrix
+ * starts on a 16-byte boundary with a row stride that is a multiple of 16 bytes, the gains need no
+ * alignment beyond their type's.  Any T >= 1 and 1 <= d <= 16384 (d need not be a multiple of anything).
+ * gate has a row per token, or with ldg = 0 one row that all tokens share.
+ *
+ * In place: h may be residual or x, y may be x or residual (same pointer, type and stride); dx, dresidual
+ * and a per-token d_gate may each be one of dy, h, dh, x, gate.  Any other overlap is refused (NPD_EINVAL).
+ *
+ * Backward (npd_norm_bwd): dy is the gradient at y (NULL if y went nowhere), dh the gradient that arrives
+ * at h from elsewhere (NULL = none); h is the forward's h (needed with dy), x, gate and the gains as in the
+ * forward; residual is not read.  NULL results are not computed.  d_gate is [T, lddg] bf16 for a
+ * per-token gate and fp32 [d], summed over the tokens, for a shared one.  The sums over tokens are taken in
+ * a fixed order: every result is bitwise reproducible.  They need a workspace of
+ * npd_norm_workspace_bytes (16-byte aligned; only read and written by the call itself; calls that share one
+ * have to follow each other); without d_*_weight and shared d_gate the workspace may be NULL.
+ */
+typedef struct npd_norm_args {
+  size_t size;               /* = sizeof(npd_norm_args); checked */
+  int32_t T, d;
+  int32_t stream_dtype, weight_dtype, flags, reserved0;
+  float eps, weight_offset, residual_scale, branch_scale;
+  const void* x;             /* bf16 [T, ldx]   */
+  const void* residual;      /* [T, ldr]        */
+  const void* gate;          /* bf16 [T, ldg], or [d] with ldg = 0 */
+  const void* post_weight;   /* [d]             */
+  const void* pre_weight;    /* [d]             */
+  void* h;                   /* [T, ldh]        output of the forward, input of the backward */
+  void* y;                   /* bf16 [T, ldy]   */
+  int64_t ldx, ldr, ldg, ldh, ldy;
+  const void* dy;            /* bf16 [T, lddy]  */
+  const void* dh;            /* [T, lddh]       */
+  void* dx;                  /* bf16 [T, lddx]  */
+  void* dresidual;           /* [T, lddr]       */
+  void* d_gate;
+  float* d_post_weight;      /* [d]             */
+  float* d_pre_weight;       /* [d]             */
+  int64_t lddy, lddh, lddx, lddr, lddg;
+  void* workspace;
+  size_t workspace_bytes;
+} npd_norm_args;
+
+int npd_norm_fwd(const npd_norm_args* args, void* cuda_stream);
+int npd_norm_bwd(const npd_norm_args* args, void* cuda_stream);
+/* HOST.  Bytes of workspace npd_norm_bwd needs (pointers inside args are not read). */
+int npd_norm_workspace_bytes(const npd_norm_args* args, size_t* out_bytes);
+
 #ifdef __cplusplus
 }
 #endif

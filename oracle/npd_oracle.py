@@ -527,3 +527,94 @@ def pack_first_fit_decreasing(lengths, keep, capacity: int):
     cu = np.concatenate([[0], np.cumsum([min(int(lengths[i]), capacity) for i in order])]).astype(np.int32)
     row_ptr = np.concatenate([[0], np.cumsum([len(m) for m in rows])]).astype(np.int32)
     return (np.asarray(order, dtype=np.int32), np.asarray(row_of, dtype=np.int32), cu, row_ptr)
+
+
+# --------------------------------------------------------------------------------------------
+# What stands around the loss step in a student: the cross-entropy of the LM head on its own, the
+# join of a block's branch with the residual stream, and a linear layer with its epilogue.
+# Definitions written out in fp64; row and column loops are left to NumPy.
+# --------------------------------------------------------------------------------------------
+def cross_entropy_step(H, W, labels, loss_mask=None, token_weight=None, tau=1.0, grad_scale=1.0):
+    """Token cross-entropy of Softmax(H W^T / tau) and the gradients of
+    grad_scale * sum_t w_t nll_t.  A token counts if its mask is set and its label lies in [0, V).
+    Returns (nll [T], lse [T], dH, dW); tokens that do not count have zeros."""
+    H, W = np.asarray(H, np.float64), np.asarray(W, np.float64)
+    T, V = H.shape[0], W.shape[0]
+    labels = np.asarray(labels)
+    on = (labels >= 0) & (labels < V)
+    if loss_mask is not None:
+        on &= np.asarray(loss_mask) != 0
+    w = np.ones(T) if token_weight is None else np.asarray(token_weight, np.float64)
+    nll, lse = np.zeros(T), np.zeros(T)
+    dH, dW = np.zeros(H.shape), np.zeros(W.shape)
+    rows = np.flatnonzero(on)
+    if rows.size == 0:
+        return nll, lse, dH, dW
+    Hr = H[rows]
+    Z = Hr @ W.T / tau
+    top = Z.max(axis=1)
+    E = np.exp(Z - top[:, None])
+    s = E.sum(axis=1)
+    lse[rows] = top + np.log(s)
+    nll[rows] = lse[rows] - Z[np.arange(rows.size), labels[rows]]
+    G = E / s[:, None]
+    G[np.arange(rows.size), labels[rows]] -= 1.0
+    G *= (grad_scale / tau * w[rows])[:, None]
+    dH[rows] = G @ W
+    dW[:] = G.T @ Hr
+    return nll, lse, dH, dW
+
+
+def _rms(v, eps):
+    return np.sqrt(np.mean(v * v, axis=1, keepdims=True) + eps)
+
+
+def norm_join(x, residual, gate=None, post_weight=None, pre_weight=None, post_norm=False, eps=1e-6,
+              weight_offset=0.0, residual_scale=1.0, branch_scale=1.0):
+    """h = residual_scale residual + branch_scale gate N(x), y = M(h), with N the norm of the branch (or
+    the identity) and M the norm in front of what reads h.  Returns (h, y)."""
+    n = 0.0
+    if x is not None:
+        n = np.asarray(x, np.float64)
+        if post_norm:
+            n = n / _rms(n, eps)
+            if post_weight is not None:
+                n = n * (np.asarray(post_weight, np.float64) + weight_offset)
+        if gate is not None:
+            n = n * np.asarray(gate, np.float64)
+    r = 0.0 if residual is None else np.asarray(residual, np.float64)
+    h = residual_scale * r + branch_scale * n
+    y = h / _rms(h, eps)
+    if pre_weight is not None:
+        y = y * (np.asarray(pre_weight, np.float64) + weight_offset)
+    return h, y
+
+
+def _rms_norm_backward(g, v, eps):
+    """Gradient at v of sum(g * v / rms(v))."""
+    r = 1.0 / _rms(v, eps)
+    return r * (g - v * r * r * np.mean(g * v, axis=1, keepdims=True))
+
+
+def norm_join_backward(dy, h, x, dh=None, gate=None, post_weight=None, pre_weight=None, post_norm=False, eps=1e-6,
+                       weight_offset=0.0, residual_scale=1.0, branch_scale=1.0):
+    """Gradients of norm_join from dy at y and dh at h; `h` is what the forward returned.  Returns a dict with
+    dx, dresidual, d_post_weight, d_pre_weight and d_gate (per token; sum it over axis 0 for a shared gate)."""
+    out = {}
+    total = 0.0 if dh is None else np.asarray(dh, np.float64)
+    if dy is not None:
+        dy, h = np.asarray(dy, np.float64), np.asarray(h, np.float64)
+        gain = 1.0 if pre_weight is None else np.asarray(pre_weight, np.float64) + weight_offset
+        total = total + _rms_norm_backward(dy * gain, h, eps)
+        out["d_pre_weight"] = np.sum(dy * h / _rms(h, eps), axis=0)
+    out["dresidual"] = residual_scale * total
+    if x is None:
+        return out
+    x = np.asarray(x, np.float64)
+    unit = x / _rms(x, eps) if post_norm else x
+    gain = 1.0 if post_weight is None or not post_norm else np.asarray(post_weight, np.float64) + weight_offset
+    out["d_gate"] = branch_scale * total * unit * gain
+    dn = branch_scale * total * (1.0 if gate is None else np.asarray(gate, np.float64))
+    out["d_post_weight"] = np.sum(dn * unit, axis=0)
+    out["dx"] = _rms_norm_backward(dn * gain, x, eps) if post_norm else dn
+    return out

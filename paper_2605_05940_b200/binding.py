@@ -7,6 +7,7 @@ PyTorch fallback: if the library is not built the first call raises.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -28,13 +29,14 @@ NPD_KD_DEBUG_CHECKS = 16
 NPD_SELECT_TEACHER_IFD_LE_1 = 1
 NPD_SELECT_SCORE_IFD_TEACHER, NPD_SELECT_SCORE_IFD_STUDENT = 2, 4
 NPD_SELECT_LO_EXCLUSIVE, NPD_SELECT_HI_EXCLUSIVE = 8, 16
+NPD_NORM_POST = 1
 NPD_GEMM_STORE_F32, NPD_GEMM_ADD_F32, NPD_GEMM_STORE_BF16, NPD_GEMM_ATOMIC_F32 = range(4)
 
 EXPORTS = ("npd_workspace_bytes", "npd_phase_count", "npd_kd_fwd_bwd", "npd_kd_fwd_bwd_host", "npd_segment_stats",
            "npd_select", "npd_last_status", "npd_strerror", "npd_last_launch_count", "npd_gemm_bf16",
            "npd_kd_forward_noalloc", "npd_pack_sequences", "npd_last_copy_bytes",
            "npd_kd_fwd_bwd_host_streams", "npd_perplexity", "npd_selftest_wait_timeout",
-           "npd_debug_chunk_schedule")
+           "npd_debug_chunk_schedule", "npd_norm_fwd", "npd_norm_bwd", "npd_norm_workspace_bytes")
 NPD_STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
 
@@ -60,6 +62,21 @@ class npd_kd_args(C.Structure):
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
         ("phase_events", C.POINTER(C.c_void_p)), ("n_phase_events", C.c_int32), ("reserved2", C.c_int32),
         ("topk_values", C.c_void_p), ("topk_indices", C.c_void_p), ("topk", C.c_int32), ("reserved3", C.c_int32),
+    ]
+
+
+class npd_norm_args(C.Structure):
+    _fields_ = [
+        ("size", C.c_size_t), ("T", C.c_int32), ("d", C.c_int32),
+        ("stream_dtype", C.c_int32), ("weight_dtype", C.c_int32), ("flags", C.c_int32), ("reserved0", C.c_int32),
+        ("eps", C.c_float), ("weight_offset", C.c_float), ("residual_scale", C.c_float), ("branch_scale", C.c_float),
+        ("x", C.c_void_p), ("residual", C.c_void_p), ("gate", C.c_void_p),
+        ("post_weight", C.c_void_p), ("pre_weight", C.c_void_p), ("h", C.c_void_p), ("y", C.c_void_p),
+        ("ldx", C.c_int64), ("ldr", C.c_int64), ("ldg", C.c_int64), ("ldh", C.c_int64), ("ldy", C.c_int64),
+        ("dy", C.c_void_p), ("dh", C.c_void_p), ("dx", C.c_void_p), ("dresidual", C.c_void_p), ("d_gate", C.c_void_p),
+        ("d_post_weight", C.c_void_p), ("d_pre_weight", C.c_void_p),
+        ("lddy", C.c_int64), ("lddh", C.c_int64), ("lddx", C.c_int64), ("lddr", C.c_int64), ("lddg", C.c_int64),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
 
@@ -100,6 +117,9 @@ def lib() -> C.CDLL:
         l.npd_gemm_bf16.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_int32,
                                     C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int64,
                                     C.c_int32, C.c_int32, C.c_void_p]
+        for f in (l.npd_norm_fwd, l.npd_norm_bwd):
+            f.argtypes = [C.POINTER(npd_norm_args), C.c_void_p]
+        l.npd_norm_workspace_bytes.argtypes = [C.POINTER(npd_norm_args), C.POINTER(C.c_size_t)]
         _lib = l
     return _lib
 
@@ -310,6 +330,191 @@ def npd_gemm_bf16(A, B, out, *, a_mn_major=False, b_mn_major=False, out_mode=NPD
                                int(b_mn_major), _ptr(out), out.stride(0), int(out_mode), int(k_splits),
                                _stream(stream)), "npd_gemm_bf16")
     return out
+
+
+# ----------------------------------------------------------------------------------------------
+# checks and allocations shared by the calls below, which take tensors and return their results
+# ----------------------------------------------------------------------------------------------
+_DT = {torch.bfloat16: NPD_DTYPE_BF16, torch.float32: NPD_DTYPE_F32}
+_BF16 = (torch.bfloat16,)
+_FLOATS = (torch.bfloat16, torch.float32)
+
+
+def _matrix(t, where, dev, rows, cols, dtypes):
+    """Checks a [rows, cols] operand on `dev` and returns its row stride (0 rows' worth is never
+    dereferenced, so one row's stride is taken as dense)."""
+    if t.device != dev or t.dtype not in dtypes:
+        raise NpdError(NPD_EINVAL, where)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise NpdError(NPD_ESHAPE, where)
+    if rows > 1:
+        return t.stride(0)
+    return (cols + 7) // 8 * 8     # a single row: its stride is never used
+
+
+def _vector(t, where, dev, n, dtypes):
+    """Checks a contiguous vector of n elements on `dev` and returns its address."""
+    if t is None:
+        return None
+    if t.device != dev or t.dtype not in dtypes:
+        raise NpdError(NPD_EINVAL, where)
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise NpdError(NPD_ESHAPE, where)
+    return t.data_ptr()
+
+
+def _cuda(t, where):
+    if t is None or not t.is_cuda:
+        raise NpdError(NPD_EINVAL, where)
+    return t.device
+
+
+def _new(rows, cols, dtype, dev):
+    """An uninitialised [rows, cols] result whose rows start on 16-byte boundaries."""
+    ld = (cols + 7) // 8 * 8
+    t = torch.empty((rows, ld), dtype=dtype, device=dev)
+    return t if ld == cols else t[:, :cols]
+
+
+_no_scope = contextlib.nullcontext()
+
+
+def _scope(dev, stream):
+    """The device of the operands current and, if a stream is given, torch's allocations on it: what a
+    call allocates belongs to the stream that the call runs on."""
+    if stream is None:
+        return _no_scope if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+    if not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    if stream.device != dev:
+        raise NpdError(NPD_EINVAL, "stream of another device")
+    return torch.cuda.stream(stream)
+
+
+def _workspace(nbytes, dev):
+    """`nbytes` of device memory, and the address of the first 1024-byte boundary in it."""
+    t = torch.empty(nbytes + 1024, dtype=torch.uint8, device=dev)
+    return t, (t.data_ptr() + 1023) & ~1023
+
+
+def _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset, residual_scale,
+               branch_scale, stream_dtype):
+    a = npd_norm_args()
+    a.size, a.T, a.d = C.sizeof(npd_norm_args), T, d
+    a.stream_dtype = _DT[stream_dtype]
+    a.flags = NPD_NORM_POST if post_norm else 0
+    a.eps, a.weight_offset, a.residual_scale, a.branch_scale = eps, weight_offset, residual_scale, branch_scale
+    w = post_weight if post_weight is not None else pre_weight
+    if w is not None:
+        if w.dtype not in _DT:
+            raise NpdError(NPD_EINVAL, where)
+        a.weight_dtype = _DT[w.dtype]
+        same = (w.dtype,)
+        a.post_weight = _vector(post_weight, where, dev, d, same)
+        a.pre_weight = _vector(pre_weight, where, dev, d, same)
+    if x is not None:
+        a.ldx, a.x = _matrix(x, where, dev, T, d, _BF16), x.data_ptr()
+    if gate is not None:
+        a.gate = gate.data_ptr()
+        if gate.dim() == 1:
+            _vector(gate, where, dev, d, _BF16)
+        else:
+            a.ldg = _matrix(gate, where, dev, T, d, _BF16)
+            if a.ldg < d:          # rows expanded from one: a shared gate is passed as a vector
+                raise NpdError(NPD_ESHAPE, where)
+    return a
+
+
+def npd_norm_fwd(x, residual=None, *, gate=None, post_weight=None, pre_weight=None, post_norm=False, eps=1e-6,
+                 weight_offset=0.0, residual_scale=1.0, branch_scale=1.0, want_h=True, want_y=True, h=None, y=None,
+                 stream=None):
+    """h = residual_scale * residual + branch_scale * gate * (norm of x, or x) and y = norm of h (see
+    npd_norm_args in include/npd.h).  x bf16 [T, d] or None, residual bf16 or f32 [T, d] or None, gate bf16
+    [d] (shared) or [T, d]; gains [d].  Results go to h and y, or to new tensors (want_h / want_y);
+    returns (h, y).  Allocations and kernels use `stream` (default: the current one)."""
+    where = "npd_norm_fwd"
+    first = x if x is not None else residual
+    dev = _cuda(first, where)
+    if first.dim() != 2:
+        raise NpdError(NPD_ESHAPE, where)
+    T, d = first.shape
+    sd = residual.dtype if residual is not None else (h.dtype if h is not None else torch.bfloat16)
+    if sd not in _DT:
+        raise NpdError(NPD_EINVAL, where)
+    with _scope(dev, stream):
+        a = _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
+                       residual_scale, branch_scale, sd)
+        if residual is not None:
+            a.ldr, a.residual = _matrix(residual, where, dev, T, d, (sd,)), residual.data_ptr()
+        if h is None and want_h:
+            h = _new(T, d, sd, dev)
+        if y is None and want_y:
+            y = _new(T, d, torch.bfloat16, dev)
+        if h is not None:
+            a.ldh, a.h = _matrix(h, where, dev, T, d, (sd,)), h.data_ptr()
+        if y is not None:
+            a.ldy, a.y = _matrix(y, where, dev, T, d, _BF16), y.data_ptr()
+        _check(lib().npd_norm_fwd(C.byref(a), _stream(None)), where)
+    return h, y
+
+
+def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_weight=None, post_norm=False, eps=1e-6,
+                 weight_offset=0.0, residual_scale=1.0, branch_scale=1.0, want_dresidual=True, want_dweights=True,
+                 dx=None, dresidual=None, workspace=None, stream=None):
+    """Gradients of npd_norm_fwd.  dy is the gradient at y (or None), h the forward's h, dh the gradient that
+    arrives at h from elsewhere (or None); the rest as in the forward.  Returns (dx, dresidual,
+    d_post_weight, d_pre_weight, d_gate), None for what has no counterpart in the call; the gradients of
+    the gains and of a shared gate are f32 [d] sums over the tokens."""
+    where = "npd_norm_bwd"
+    first = dy if dy is not None else dh
+    dev = _cuda(first, where)
+    if first.dim() != 2:
+        raise NpdError(NPD_ESHAPE, where)
+    T, d = first.shape
+    sd = next((t.dtype for t in (h, dh, dresidual) if t is not None), torch.bfloat16)
+    if sd not in _DT:
+        raise NpdError(NPD_EINVAL, where)
+    with _scope(dev, stream):
+        a = _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
+                       residual_scale, branch_scale, sd)
+        if dy is not None:
+            a.lddy, a.dy = _matrix(dy, where, dev, T, d, _BF16), dy.data_ptr()
+        if h is not None:
+            a.ldh, a.h = _matrix(h, where, dev, T, d, (sd,)), h.data_ptr()
+        if dh is not None:
+            a.lddh, a.dh = _matrix(dh, where, dev, T, d, (sd,)), dh.data_ptr()
+        if dx is None and x is not None:
+            dx = _new(T, d, torch.bfloat16, dev)
+        if dresidual is None and want_dresidual:
+            dresidual = _new(T, d, sd, dev)
+        if dx is not None:
+            a.lddx, a.dx = _matrix(dx, where, dev, T, d, _BF16), dx.data_ptr()
+        if dresidual is not None:
+            a.lddr, a.dresidual = _matrix(dresidual, where, dev, T, d, (sd,)), dresidual.data_ptr()
+        d_post = d_pre = d_gate = None
+        if want_dweights and post_norm and post_weight is not None:
+            d_post = torch.empty(d, dtype=torch.float32, device=dev)
+            a.d_post_weight = d_post.data_ptr()
+        if want_dweights and pre_weight is not None and dy is not None:
+            d_pre = torch.empty(d, dtype=torch.float32, device=dev)
+            a.d_pre_weight = d_pre.data_ptr()
+        if gate is not None:
+            if gate.dim() == 1:
+                d_gate = torch.empty(d, dtype=torch.float32, device=dev)
+            else:
+                d_gate = _new(T, d, torch.bfloat16, dev)
+                a.lddg = _matrix(d_gate, where, dev, T, d, _BF16)
+            a.d_gate = d_gate.data_ptr()
+        if d_post is not None or d_pre is not None or (d_gate is not None and gate.dim() == 1):
+            if workspace is None:
+                n = C.c_size_t(0)
+                _check(lib().npd_norm_workspace_bytes(C.byref(a), C.byref(n)), where)
+                workspace, a.workspace = _workspace(n.value, dev)
+                a.workspace_bytes = n.value
+            else:
+                a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib().npd_norm_bwd(C.byref(a), _stream(None)), where)
+    return dx, dresidual, d_post, d_pre, d_gate
 
 
 class KDStep:

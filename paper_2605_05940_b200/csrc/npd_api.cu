@@ -938,3 +938,5 @@ int npd_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, i
 }
 
 }  // extern "C"
+
+#include "norm_api.cuh"
