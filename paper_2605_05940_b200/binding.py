@@ -333,47 +333,57 @@ def npd_gemm_bf16(A, B, out, *, a_mn_major=False, b_mn_major=False, out_mode=NPD
 
 
 # ----------------------------------------------------------------------------------------------
-# checks and allocations shared by the calls below, which take tensors and return their results
+# Checks and allocations shared by the calls below, which take tensors and return their results.
+# Written for little host time: a call on a small problem is bound by what Python does around it.
 # ----------------------------------------------------------------------------------------------
 _DT = {torch.bfloat16: NPD_DTYPE_BF16, torch.float32: NPD_DTYPE_F32}
-_BF16 = (torch.bfloat16,)
-_FLOATS = (torch.bfloat16, torch.float32)
+_raw_stream = torch._C._cuda_getCurrentRawStream if hasattr(torch._C, "_cuda_getCurrentRawStream") else None
 
 
-def _matrix(t, where, dev, rows, cols, dtypes):
-    """Checks a [rows, cols] operand on `dev` and returns its row stride (0 rows' worth is never
-    dereferenced, so one row's stride is taken as dense)."""
-    if t.device != dev or t.dtype not in dtypes:
+def _device_of(t, where):
+    """Index of the GPU that holds t; a missing tensor or one elsewhere is refused."""
+    if t is None or not t.is_cuda:
         raise NpdError(NPD_EINVAL, where)
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    return t.get_device()
+
+
+def _matrix(t, where, dev, shape, dtype):
+    """Checks an operand of this shape and type on GPU `dev` and returns its row stride."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise NpdError(NPD_EINVAL, where)
+    if t.shape != shape:
         raise NpdError(NPD_ESHAPE, where)
-    if rows > 1:
-        return t.stride(0)
-    return (cols + 7) // 8 * 8     # a single row: its stride is never used
+    rows, cols = shape
+    s = t.stride()
+    if cols > 1 and s[1] != 1:
+        raise NpdError(NPD_ESHAPE, where)
+    return s[0] if rows > 1 else (cols + 7) // 8 * 8     # the stride of a single row is never used
 
 
-def _vector(t, where, dev, n, dtypes):
-    """Checks a contiguous vector of n elements on `dev` and returns its address."""
+def _vector(t, where, dev, n, dtype):
+    """Checks a contiguous vector of n elements on GPU `dev` and returns its address."""
     if t is None:
         return None
-    if t.device != dev or t.dtype not in dtypes:
+    if t.dtype is not dtype or t.get_device() != dev:
         raise NpdError(NPD_EINVAL, where)
     if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
         raise NpdError(NPD_ESHAPE, where)
     return t.data_ptr()
 
 
-def _cuda(t, where):
-    if t is None or not t.is_cuda:
-        raise NpdError(NPD_EINVAL, where)
-    return t.device
+def _new(shape, dtype, device):
+    """An uninitialised matrix whose rows start on 16-byte boundaries."""
+    cols = shape[1]
+    if cols % 8 == 0:
+        return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty((shape[0], (cols + 7) // 8 * 8), dtype=dtype, device=device)[:, :cols]
 
 
-def _new(rows, cols, dtype, dev):
-    """An uninitialised [rows, cols] result whose rows start on 16-byte boundaries."""
-    ld = (cols + 7) // 8 * 8
-    t = torch.empty((rows, ld), dtype=dtype, device=dev)
-    return t if ld == cols else t[:, :cols]
+def _like(t, shape, dtype):
+    """_new(...) on t's GPU; quicker where t itself has that shape and type and is dense."""
+    if t is not None and t.dtype is dtype and shape[1] % 8 == 0 and t.is_contiguous():
+        return torch.empty_like(t)
+    return None if t is None else _new(shape, dtype, t.device)
 
 
 _no_scope = contextlib.nullcontext()
@@ -383,43 +393,43 @@ def _scope(dev, stream):
     """The device of the operands current and, if a stream is given, torch's allocations on it: what a
     call allocates belongs to the stream that the call runs on."""
     if stream is None:
-        return _no_scope if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
+        return _no_scope if dev == torch.cuda.current_device() else torch.cuda.device(dev)
     if not hasattr(stream, "cuda_stream"):
         stream = torch.cuda.ExternalStream(int(stream), device=dev)
-    if stream.device != dev:
+    if stream.device.index != dev:
         raise NpdError(NPD_EINVAL, "stream of another device")
     return torch.cuda.stream(stream)
 
 
-def _workspace(nbytes, dev):
+def _current(dev):
+    """Handle of torch's current stream on GPU `dev`."""
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _workspace(nbytes, device):
     """`nbytes` of device memory, and the address of the first 1024-byte boundary in it."""
-    t = torch.empty(nbytes + 1024, dtype=torch.uint8, device=dev)
+    t = torch.empty(nbytes + 1024, dtype=torch.uint8, device=device)
     return t, (t.data_ptr() + 1023) & ~1023
 
 
-def _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset, residual_scale,
+def _norm_args(where, dev, shape, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset, residual_scale,
                branch_scale, stream_dtype):
-    a = npd_norm_args()
-    a.size, a.T, a.d = C.sizeof(npd_norm_args), T, d
-    a.stream_dtype = _DT[stream_dtype]
-    a.flags = NPD_NORM_POST if post_norm else 0
-    a.eps, a.weight_offset, a.residual_scale, a.branch_scale = eps, weight_offset, residual_scale, branch_scale
+    T, d = shape
     w = post_weight if post_weight is not None else pre_weight
+    if stream_dtype not in _DT or (w is not None and w.dtype not in _DT):
+        raise NpdError(NPD_EINVAL, where)
+    a = npd_norm_args(C.sizeof(npd_norm_args), T, d, _DT[stream_dtype], 0 if w is None else _DT[w.dtype],
+                      NPD_NORM_POST if post_norm else 0, 0, eps, weight_offset, residual_scale, branch_scale)
     if w is not None:
-        if w.dtype not in _DT:
-            raise NpdError(NPD_EINVAL, where)
-        a.weight_dtype = _DT[w.dtype]
-        same = (w.dtype,)
-        a.post_weight = _vector(post_weight, where, dev, d, same)
-        a.pre_weight = _vector(pre_weight, where, dev, d, same)
+        a.post_weight = _vector(post_weight, where, dev, d, w.dtype)
+        a.pre_weight = _vector(pre_weight, where, dev, d, w.dtype)
     if x is not None:
-        a.ldx, a.x = _matrix(x, where, dev, T, d, _BF16), x.data_ptr()
+        a.ldx, a.x = _matrix(x, where, dev, shape, torch.bfloat16), x.data_ptr()
     if gate is not None:
-        a.gate = gate.data_ptr()
         if gate.dim() == 1:
-            _vector(gate, where, dev, d, _BF16)
+            a.gate = _vector(gate, where, dev, d, torch.bfloat16)
         else:
-            a.ldg = _matrix(gate, where, dev, T, d, _BF16)
+            a.ldg, a.gate = _matrix(gate, where, dev, shape, torch.bfloat16), gate.data_ptr()
             if a.ldg < d:          # rows expanded from one: a shared gate is passed as a vector
                 raise NpdError(NPD_ESHAPE, where)
     return a
@@ -434,27 +444,25 @@ def npd_norm_fwd(x, residual=None, *, gate=None, post_weight=None, pre_weight=No
     returns (h, y).  Allocations and kernels use `stream` (default: the current one)."""
     where = "npd_norm_fwd"
     first = x if x is not None else residual
-    dev = _cuda(first, where)
-    if first.dim() != 2:
+    dev = _device_of(first, where)
+    shape = first.shape
+    if len(shape) != 2:
         raise NpdError(NPD_ESHAPE, where)
-    T, d = first.shape
     sd = residual.dtype if residual is not None else (h.dtype if h is not None else torch.bfloat16)
-    if sd not in _DT:
-        raise NpdError(NPD_EINVAL, where)
     with _scope(dev, stream):
-        a = _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
+        a = _norm_args(where, dev, shape, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
                        residual_scale, branch_scale, sd)
         if residual is not None:
-            a.ldr, a.residual = _matrix(residual, where, dev, T, d, (sd,)), residual.data_ptr()
+            a.ldr, a.residual = _matrix(residual, where, dev, shape, sd), residual.data_ptr()
         if h is None and want_h:
-            h = _new(T, d, sd, dev)
+            h = _like(residual if residual is not None else first, shape, sd)
         if y is None and want_y:
-            y = _new(T, d, torch.bfloat16, dev)
+            y = _like(first, shape, torch.bfloat16)
         if h is not None:
-            a.ldh, a.h = _matrix(h, where, dev, T, d, (sd,)), h.data_ptr()
+            a.ldh, a.h = _matrix(h, where, dev, shape, sd), h.data_ptr()
         if y is not None:
-            a.ldy, a.y = _matrix(y, where, dev, T, d, _BF16), y.data_ptr()
-        _check(lib().npd_norm_fwd(C.byref(a), _stream(None)), where)
+            a.ldy, a.y = _matrix(y, where, dev, shape, torch.bfloat16), y.data_ptr()
+        _check(lib().npd_norm_fwd(a, _current(dev)), where)
     return h, y
 
 
@@ -467,53 +475,54 @@ def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_wei
     the gains and of a shared gate are f32 [d] sums over the tokens."""
     where = "npd_norm_bwd"
     first = dy if dy is not None else dh
-    dev = _cuda(first, where)
-    if first.dim() != 2:
+    dev = _device_of(first, where)
+    shape, device = first.shape, first.device
+    if len(shape) != 2:
         raise NpdError(NPD_ESHAPE, where)
-    T, d = first.shape
+    T, d = shape
     sd = next((t.dtype for t in (h, dh, dresidual) if t is not None), torch.bfloat16)
-    if sd not in _DT:
-        raise NpdError(NPD_EINVAL, where)
+    bf16 = torch.bfloat16
     with _scope(dev, stream):
-        a = _norm_args(where, dev, T, d, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
+        a = _norm_args(where, dev, shape, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset,
                        residual_scale, branch_scale, sd)
         if dy is not None:
-            a.lddy, a.dy = _matrix(dy, where, dev, T, d, _BF16), dy.data_ptr()
+            a.lddy, a.dy = _matrix(dy, where, dev, shape, bf16), dy.data_ptr()
         if h is not None:
-            a.ldh, a.h = _matrix(h, where, dev, T, d, (sd,)), h.data_ptr()
+            a.ldh, a.h = _matrix(h, where, dev, shape, sd), h.data_ptr()
         if dh is not None:
-            a.lddh, a.dh = _matrix(dh, where, dev, T, d, (sd,)), dh.data_ptr()
+            a.lddh, a.dh = _matrix(dh, where, dev, shape, sd), dh.data_ptr()
         if dx is None and x is not None:
-            dx = _new(T, d, torch.bfloat16, dev)
+            dx = _like(x, shape, bf16)
         if dresidual is None and want_dresidual:
-            dresidual = _new(T, d, sd, dev)
+            dresidual = _like(dh if dh is not None else first, shape, sd)
         if dx is not None:
-            a.lddx, a.dx = _matrix(dx, where, dev, T, d, _BF16), dx.data_ptr()
+            a.lddx, a.dx = _matrix(dx, where, dev, shape, bf16), dx.data_ptr()
         if dresidual is not None:
-            a.lddr, a.dresidual = _matrix(dresidual, where, dev, T, d, (sd,)), dresidual.data_ptr()
+            a.lddr, a.dresidual = _matrix(dresidual, where, dev, shape, sd), dresidual.data_ptr()
         d_post = d_pre = d_gate = None
         if want_dweights and post_norm and post_weight is not None:
-            d_post = torch.empty(d, dtype=torch.float32, device=dev)
+            d_post = torch.empty(d, dtype=torch.float32, device=device)
             a.d_post_weight = d_post.data_ptr()
         if want_dweights and pre_weight is not None and dy is not None:
-            d_pre = torch.empty(d, dtype=torch.float32, device=dev)
+            d_pre = torch.empty(d, dtype=torch.float32, device=device)
             a.d_pre_weight = d_pre.data_ptr()
+        shared = gate is not None and gate.dim() == 1
         if gate is not None:
-            if gate.dim() == 1:
-                d_gate = torch.empty(d, dtype=torch.float32, device=dev)
+            if shared:
+                d_gate = torch.empty(d, dtype=torch.float32, device=device)
             else:
-                d_gate = _new(T, d, torch.bfloat16, dev)
-                a.lddg = _matrix(d_gate, where, dev, T, d, _BF16)
+                d_gate = _new(shape, bf16, device)
+                a.lddg = _matrix(d_gate, where, dev, shape, bf16)
             a.d_gate = d_gate.data_ptr()
-        if d_post is not None or d_pre is not None or (d_gate is not None and gate.dim() == 1):
+        if d_post is not None or d_pre is not None or shared:
             if workspace is None:
                 n = C.c_size_t(0)
-                _check(lib().npd_norm_workspace_bytes(C.byref(a), C.byref(n)), where)
-                workspace, a.workspace = _workspace(n.value, dev)
+                _check(lib().npd_norm_workspace_bytes(a, n), where)
+                workspace, a.workspace = _workspace(n.value, device)
                 a.workspace_bytes = n.value
             else:
                 a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-        _check(lib().npd_norm_bwd(C.byref(a), _stream(None)), where)
+        _check(lib().npd_norm_bwd(a, _current(dev)), where)
     return dx, dresidual, d_post, d_pre, d_gate
 
 
