@@ -405,6 +405,71 @@ int npd_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, i
                   const void* B, int64_t ldb, int32_t b_mn_major, void* out, int64_t ldo,
                   int32_t out_mode, int32_t k_splits, void* cuda_stream);
 
+/* flags of npd_ce_args */
+enum {
+  NPD_CE_ACCUMULATE_DW = 1,     /* add into d_weight instead of overwriting it (f32 d_weight only) */
+  NPD_CE_SERIALIZE_LAUNCHES = 2 /* no programmatic dependent launches (see NPD_KD_SERIALIZE_LAUNCHES) */
+};
+
+/*
+ * Token cross-entropy of the LM head on its own (the L_CE of Eq. 1 and the sequence losses behind
+ * Eq. 3), with its gradient, without a teacher and without the [T, V] logits in memory:
+ *
+ *   z[t,c]  = <hidden[t], weight[c]> / temperature
+ *   lse[t]  = log sum_c exp z[t,c]
+ *   nll[t]  = lse[t] - z[t, y_t]
+ *   dz[t,c] = grad_scale * w_t * (exp(z[t,c] - lse[t]) - [c = y_t])
+ *   d_hidden = dz weight / temperature,   d_weight = dz^T hidden / temperature
+ *
+ * the gradient of grad_scale * sum_t w_t nll[t].  A token counts if its mask is set and its label
+ * lies in [0, V); the others have nll = lse = 0, no gradient (zero rows in d_hidden), and their hidden
+ * states are never read.  Every output element is written.  A non-finite hidden state makes that token's
+ * loss and row of d_hidden, and all of d_weight, NaN.
+ *
+ * With d_hidden = d_weight = NULL only the losses are computed: the scoring pass of the Delta-IFD filter
+ * (npd_segment_stats takes nll in the place of either model's), from one token to a full batch.
+ * Either gradient may be NULL (a frozen head, for instance); the work for it is then left out.
+ *
+ * Layouts and alignment as in npd_kd_args: row-major, row strides in ELEMENTS, the four matrices 16-byte
+ * aligned with row strides that are multiples of 16 bytes, d a multiple of 64, any T >= 1, V >= 1.  Outputs may not
+ * overlap inputs or each other (NPD_EINVAL).
+ *
+ * nll, lse and d_weight are bitwise reproducible; d_hidden is summed over pieces of the vocabulary with
+ * fp32 atomic adds whose order is not fixed (a few of its bf16 elements may round differently).  The logit
+ * gradients are rounded to bf16 (without grad_scale) on the way to the two products: an fp32 d_weight
+ * has fp32 sums of bf16-rounded terms.
+ *
+ * The workspace belongs to one call at a time: calls that share one have to follow each other, captured
+ * graphs among them.  Device-side errors (a wait that ran out) are read with npd_last_status.
+ */
+typedef struct npd_ce_args {
+  size_t size;               /* = sizeof(npd_ce_args); checked */
+  int32_t T, d, V, flags;
+  const void* hidden;        /* bf16 [T, ldh] */
+  const void* weight;        /* bf16 [V, ldw] */
+  int64_t ldh, ldw;
+  const int32_t* labels;     /* [T] */
+  const uint8_t* loss_mask;  /* [T] or NULL = all ones */
+  const float* token_weight; /* [T] w_t, or NULL = 1 */
+  float temperature;         /* > 0 */
+  float grad_scale;
+  float* nll;                /* [T] required */
+  float* lse;                /* [T] or NULL  */
+  void* d_hidden;            /* bf16 [T, ld_dh] or NULL */
+  void* d_weight;            /* bf16 or f32 [V, ld_dw] or NULL */
+  int64_t ld_dh, ld_dw;
+  int32_t d_weight_dtype;
+  int32_t grad_chunk_cols;   /* vocabulary columns of logit gradients in the workspace at a time (rounded up
+                                to a multiple of 256); 0 = library default */
+  void* workspace;           /* >= npd_ce_workspace_bytes(), 1024-byte aligned */
+  size_t workspace_bytes;
+} npd_ce_args;
+
+/* HOST.  Bytes of workspace for these arguments (of the pointers only the presence of d_hidden and
+ * d_weight matters). */
+int npd_ce_workspace_bytes(const npd_ce_args* args, size_t* out_bytes);
+int npd_ce_fwd_bwd(const npd_ce_args* args, void* cuda_stream);
+
 /* flags of npd_norm_args */
 enum { NPD_NORM_POST = 1 /* the branch goes through a norm of its own before it is added */ };
 

@@ -30,13 +30,15 @@ NPD_SELECT_TEACHER_IFD_LE_1 = 1
 NPD_SELECT_SCORE_IFD_TEACHER, NPD_SELECT_SCORE_IFD_STUDENT = 2, 4
 NPD_SELECT_LO_EXCLUSIVE, NPD_SELECT_HI_EXCLUSIVE = 8, 16
 NPD_NORM_POST = 1
+NPD_CE_ACCUMULATE_DW, NPD_CE_SERIALIZE_LAUNCHES = 1, 2
 NPD_GEMM_STORE_F32, NPD_GEMM_ADD_F32, NPD_GEMM_STORE_BF16, NPD_GEMM_ATOMIC_F32 = range(4)
 
 EXPORTS = ("npd_workspace_bytes", "npd_phase_count", "npd_kd_fwd_bwd", "npd_kd_fwd_bwd_host", "npd_segment_stats",
            "npd_select", "npd_last_status", "npd_strerror", "npd_last_launch_count", "npd_gemm_bf16",
            "npd_kd_forward_noalloc", "npd_pack_sequences", "npd_last_copy_bytes",
            "npd_kd_fwd_bwd_host_streams", "npd_perplexity", "npd_selftest_wait_timeout",
-           "npd_debug_chunk_schedule", "npd_norm_fwd", "npd_norm_bwd", "npd_norm_workspace_bytes")
+           "npd_debug_chunk_schedule", "npd_norm_fwd", "npd_norm_bwd", "npd_norm_workspace_bytes",
+           "npd_ce_fwd_bwd", "npd_ce_workspace_bytes")
 NPD_STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
 
@@ -76,6 +78,19 @@ class npd_norm_args(C.Structure):
         ("dy", C.c_void_p), ("dh", C.c_void_p), ("dx", C.c_void_p), ("dresidual", C.c_void_p), ("d_gate", C.c_void_p),
         ("d_post_weight", C.c_void_p), ("d_pre_weight", C.c_void_p),
         ("lddy", C.c_int64), ("lddh", C.c_int64), ("lddx", C.c_int64), ("lddr", C.c_int64), ("lddg", C.c_int64),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class npd_ce_args(C.Structure):
+    _fields_ = [
+        ("size", C.c_size_t), ("T", C.c_int32), ("d", C.c_int32), ("V", C.c_int32), ("flags", C.c_int32),
+        ("hidden", C.c_void_p), ("weight", C.c_void_p), ("ldh", C.c_int64), ("ldw", C.c_int64),
+        ("labels", C.c_void_p), ("loss_mask", C.c_void_p), ("token_weight", C.c_void_p),
+        ("temperature", C.c_float), ("grad_scale", C.c_float),
+        ("nll", C.c_void_p), ("lse", C.c_void_p), ("d_hidden", C.c_void_p), ("d_weight", C.c_void_p),
+        ("ld_dh", C.c_int64), ("ld_dw", C.c_int64),
+        ("d_weight_dtype", C.c_int32), ("grad_chunk_cols", C.c_int32),
         ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
     ]
 
@@ -120,6 +135,8 @@ def lib() -> C.CDLL:
         for f in (l.npd_norm_fwd, l.npd_norm_bwd):
             f.argtypes = [C.POINTER(npd_norm_args), C.c_void_p]
         l.npd_norm_workspace_bytes.argtypes = [C.POINTER(npd_norm_args), C.POINTER(C.c_size_t)]
+        l.npd_ce_fwd_bwd.argtypes = [C.POINTER(npd_ce_args), C.c_void_p]
+        l.npd_ce_workspace_bytes.argtypes = [C.POINTER(npd_ce_args), C.POINTER(C.c_size_t)]
         _lib = l
     return _lib
 
@@ -524,6 +541,82 @@ def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_wei
                 a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         _check(lib().npd_norm_bwd(a, _current(dev)), where)
     return dx, dresidual, d_post, d_pre, d_gate
+
+
+class CEStep:
+    """Cross-entropy of the LM head for one set of tensors: checks them, holds the results (nll, lse,
+    d_hidden, d_weight) and the workspace, and runs the step on them; see npd_ce_args in include/npd.h.
+
+    hidden bf16 [T, d], weight bf16 [V, d], labels int32 [T], loss_mask uint8 or bool [T], token_weight f32 [T].
+    d_hidden / d_weight: True for a new tensor, None for none, or a tensor to write to (an f32 d_weight with
+    accumulate_dw is added to).  The tensors are allocated on `stream` (default: the current one)."""
+
+    def __init__(self, hidden, weight, labels, *, loss_mask=None, token_weight=None, temperature=1.0, grad_scale=1.0,
+                 d_hidden=True, d_weight=True, dw_dtype=torch.bfloat16, accumulate_dw=False, want_lse=True,
+                 grad_chunk_cols=0, flags=0, workspace=None, stream=None):
+        where = "npd_ce_fwd_bwd"
+        dev = self._dev = _device_of(hidden, where)
+        if hidden.dim() != 2 or weight.dim() != 2:
+            raise NpdError(NPD_ESHAPE, where)
+        shape, device, bf16 = hidden.shape, hidden.device, torch.bfloat16
+        T, d = shape
+        V = weight.shape[0]
+        a = self.args = npd_ce_args(C.sizeof(npd_ce_args), T, d, V, flags | (NPD_CE_ACCUMULATE_DW if accumulate_dw else 0))
+        # what the step reads is kept alive as long as the step is
+        self._inputs = (hidden, weight, labels, loss_mask, token_weight)
+        with _scope(dev, stream):
+            a.ldh, a.hidden = _matrix(hidden, where, dev, shape, bf16), hidden.data_ptr()
+            a.ldw, a.weight = _matrix(weight, where, dev, (V, d), bf16), weight.data_ptr()
+            a.labels = _vector(labels, where, dev, T, torch.int32)
+            if loss_mask is not None:
+                a.loss_mask = _vector(loss_mask, where, dev, T, torch.bool if loss_mask.dtype is torch.bool else torch.uint8)
+            a.token_weight = _vector(token_weight, where, dev, T, torch.float32)
+            a.temperature, a.grad_scale, a.grad_chunk_cols = temperature, grad_scale, grad_chunk_cols
+            self.nll = torch.empty(T, dtype=torch.float32, device=device)
+            self.lse = torch.empty(T, dtype=torch.float32, device=device) if want_lse else None
+            a.nll, a.lse = self.nll.data_ptr(), _ptr(self.lse)
+            if d_hidden is True:
+                d_hidden = _like(hidden, shape, bf16)
+            if d_weight is True:
+                d_weight = _new((V, d), dw_dtype, device)
+            self.d_hidden, self.d_weight = d_hidden, d_weight
+            if d_hidden is not None:
+                a.ld_dh, a.d_hidden = _matrix(d_hidden, where, dev, shape, bf16), d_hidden.data_ptr()
+            if d_weight is not None:
+                if d_weight.dtype not in _DT:
+                    raise NpdError(NPD_EINVAL, where)
+                a.ld_dw, a.d_weight = _matrix(d_weight, where, dev, (V, d), d_weight.dtype), d_weight.data_ptr()
+                a.d_weight_dtype = _DT[d_weight.dtype]
+            if workspace is None:
+                n = C.c_size_t(0)
+                _check(lib().npd_ce_workspace_bytes(a, n), where)
+                self._workspace, a.workspace = _workspace(n.value, device)
+                a.workspace_bytes = n.value
+            else:
+                self._workspace, a.workspace = workspace, workspace.data_ptr()
+                a.workspace_bytes = workspace.numel() * workspace.element_size()
+
+    def run(self, stream=None):
+        """Enqueues the step on `stream` (default: the current one of the tensors' GPU)."""
+        with _scope(self._dev, stream):
+            _check(lib().npd_ce_fwd_bwd(self.args, _current(self._dev)), "npd_ce_fwd_bwd")
+
+    def status(self, stream=None) -> int:
+        """Waits for `stream` and returns the status that the step's kernels left in the workspace."""
+        out = C.c_int32(0)
+        with _scope(self._dev, stream):
+            _check(lib().npd_last_status(self.args.workspace, _current(self._dev), C.byref(out)), "npd_last_status")
+        return out.value
+
+
+def npd_cross_entropy(hidden, weight, labels, *, grads=True, stream=None, **kw):
+    """One cross-entropy step with new results: (nll, lse, d_hidden, d_weight), the gradients None without
+    `grads`.  Further arguments as for CEStep, which a loop over fixed buffers uses instead."""
+    if not grads:
+        kw["d_hidden"] = kw["d_weight"] = None
+    s = CEStep(hidden, weight, labels, stream=stream, **kw)
+    s.run(stream)
+    return s.nll, s.lse, s.d_hidden, s.d_weight
 
 
 class KDStep:

@@ -1,0 +1,391 @@
+// Token cross-entropy of an LM head over a large vocabulary, and its gradient, without the [T, V]
+// logits in memory:
+//
+//   z = H W^T / tau,  lse[t] = log sum_c exp z[t,c],  nll[t] = lse[t] - z[t, y_t]
+//   dH = s (G W),  dW = s (G^T H),  G[t,c] = w_t (exp(z[t,c] - lse[t]) - [c = y_t]),  s = grad_scale / tau
+//
+// The tokens that count (mask set, label inside the vocabulary) are numbered and their hidden states
+// gathered ("compact rows"); everything below works on those only.  Tensor-core tiles (pair_tile_sm100.cuh)
+// form the logits twice: the forward tiles keep a running maximum and sum per row over a run of
+// vocabulary tiles, and pick out the label's logit; the gradient tiles write G, in bf16, for one
+// piece of the vocabulary at a time, and two contractions add the piece to dH and give its rows of dW.
+// Logits are recomputed rather than kept: 8 d V operations per token for a method of 6 d V.
+//
+// Roundings: logits, maxima, sums and losses are fp32.  G is rounded to bf16 because the contractions'
+// operands are; it holds w_t (p - [c = y]) without the scale s, which the contractions' epilogues
+// multiply in fp32, so the label's entry is -1 but for a small p (exact in bf16 for w_t = 1) instead of
+// one common rounding error of s in every token.
+#pragma once
+
+#include "pair_tile_sm100.cuh"
+#include "small_kernels.cuh"
+
+namespace npd {
+
+struct CePlanParams {
+  int T, V, d;
+  const uint8_t* mask;     // or NULL
+  const int32_t* labels;
+  const float* weight;     // token weights, or NULL
+  const __nv_bfloat16* hidden;
+  const __nv_bfloat16* head;
+  long long ldh, ldw;
+  float scale2;            // log2(e) / tau
+  int vtiles, nsplit_max, clusters;
+  int* plan;               // {blocks, pairs of blocks, forward runs, Tc}
+  int* cidx;               // [T] compact row of a token, or -1
+  int* cy;                 // [blocks*128] label of a compact row (-1 beyond Tc)
+  float* cw;               // [blocks*128] weight of a compact row (0 beyond Tc)
+  float* zy;               // [blocks*128] the label's scaled logit, summed in fp32 (see ce_merge_kernel)
+  __nv_bfloat16* hc;       // [blocks*128, d] hidden states of the compact rows (0 beyond Tc)
+  float* dh_acc;           // [blocks*128, d], cleared here; or NULL
+  int* status;
+};
+
+__device__ __forceinline__ bool ce_counts(const CePlanParams& p, int t) {
+  if (p.mask != nullptr && p.mask[t] == 0) return false;
+  const int y = p.labels[t];
+  return y >= 0 && y < p.V;
+}
+
+// Numbers the tokens that count, in packed order, and gathers what the tiles read.  Every CTA handles a
+// stretch of tokens; it counts the ones before its stretch itself (5 bytes per token, from L2), which
+// saves a second launch.  CTA 0 counts all of them and writes the plan and the padding rows.
+__global__ void __launch_bounds__(1024) ce_plan_kernel(const CePlanParams p) {
+  __shared__ int warp_n[32];
+  __shared__ int total_s;
+  __shared__ int list[1024];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  // stretches are whole multiples of 8 tokens
+  const int per = ((p.T + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x) + 7) / 8 * 8;
+  const int t0 = static_cast<int>(min(static_cast<long long>(p.T), static_cast<long long>(blockIdx.x) * per));
+  const int t1 = min(p.T, t0 + per);
+  // tokens that count before t0 (CTA 0: in the whole batch)
+  const int upto = blockIdx.x == 0 ? p.T : t0;
+  int n = 0;
+  for (int t = threadIdx.x; t < upto; t += blockDim.x) n += ce_counts(p, t) ? 1 : 0;
+  n = warp_sum_int(n);
+  if (lane == 0) warp_n[warp] = n;
+  __syncthreads();
+  if (warp == 0) {
+    n = warp_sum_int(warp_n[lane]);
+    if (lane == 0) total_s = n;
+  }
+  __syncthreads();
+  int base = blockIdx.x == 0 ? 0 : total_s;
+  const int tc = total_s;  // meaningful in CTA 0 only
+  const int per_row = p.d / 8;
+  for (int c0 = t0; c0 < t1; c0 += 1024) {
+    const int t = c0 + threadIdx.x;
+    const bool on = t < t1 && ce_counts(p, t);
+    const unsigned votes = __ballot_sync(0xffffffffu, on);
+    __syncthreads();  // the list and the warp counts of the round before have been read
+    if (lane == 0) warp_n[warp] = __popc(votes);
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int w = 0; w < 32; ++w) {
+      before += w < warp ? warp_n[w] : 0;
+      all += warp_n[w];
+    }
+    const int at = before + __popc(votes & ((1u << lane) - 1u));
+    if (t < t1) p.cidx[t] = on ? base + at : -1;
+    if (on) {
+      list[at] = t;
+      p.cy[base + at] = p.labels[t];
+      p.cw[base + at] = p.weight != nullptr ? p.weight[t] : 1.f;
+    }
+    __syncthreads();
+    for (long long i = threadIdx.x; i < static_cast<long long>(all) * per_row; i += blockDim.x) {
+      const int r = static_cast<int>(i / per_row), k = static_cast<int>(i % per_row) * 8;
+      const size_t c = static_cast<size_t>(base + r) * p.d + k;
+      *reinterpret_cast<uint4*>(p.hc + c) =
+          *reinterpret_cast<const uint4*>(p.hidden + static_cast<size_t>(list[r]) * p.ldh + k);
+      if (p.dh_acc != nullptr) {
+        reinterpret_cast<float4*>(p.dh_acc + c)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+        reinterpret_cast<float4*>(p.dh_acc + c)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+    for (int r = warp; r < all; r += 32) {
+      const int t = list[r];
+      const float z = warp_dot_bf16(p.hidden + static_cast<size_t>(t) * p.ldh,
+                                    p.head + static_cast<size_t>(p.labels[t]) * p.ldw, p.d, lane);
+      if (lane == 0) p.zy[base + r] = z * p.scale2;
+    }
+    base += all;
+  }
+  if (blockIdx.x != 0) return;
+  const int nact = (tc + 127) / 128, pairs = (nact + 1) / 2;
+  for (int i = tc + threadIdx.x; i < nact * 128; i += blockDim.x) {
+    p.cy[i] = -1;
+    p.cw[i] = 0.f;
+  }
+  for (long long i = threadIdx.x; i < static_cast<long long>(nact * 128 - tc) * per_row; i += blockDim.x) {
+    const size_t c = static_cast<size_t>(tc) * p.d + static_cast<size_t>(i) * 8;
+    *reinterpret_cast<uint4*>(p.hc + c) = make_uint4(0u, 0u, 0u, 0u);
+    if (p.dh_acc != nullptr) {
+      reinterpret_cast<float4*>(p.dh_acc + c)[0] = make_float4(0.f, 0.f, 0.f, 0.f);
+      reinterpret_cast<float4*>(p.dh_acc + c)[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  if (threadIdx.x == 0) {
+    p.plan[0] = nact;
+    p.plan[1] = pairs;
+    p.plan[2] = choose_nsplit(pairs > 0 ? pairs : 1, p.vtiles, p.clusters, p.nsplit_max);
+    p.plan[3] = tc;
+    *p.status = 0;
+  }
+}
+
+struct CeTileParams {
+  int V, ksteps;
+  const int* plan;
+  const int* cy;       // [blocks*128]
+  const float* cw;     // [blocks*128]
+  int group_pairs;     // pairs of row blocks per group (see CeWalk)
+  int vt_begin, vt_count;
+  float scale2;        // log2(e) / tau
+  long long rows;      // stride of the partials: compact rows the workspace has room for
+  float2* partials;    // forward: [2 * runs][rows] {maximum, sum}, base 2, logits scaled by scale2
+  float* zlabel;       // forward: [rows] the label's scaled logit
+  const float* lse2;   // gradient: [rows] log2-sum-exp2 of the scaled logits
+  int g_col0;          // gradient: vocabulary column of the scratch's column 0
+  int* status;
+};
+
+// Units of (pair of row blocks, run of vocabulary tiles), dealt round robin.  They are ordered in
+// groups of pairs whose hidden states fit a quarter of L2 (within a group the pair varies fastest, then
+// the run), so the pairs that work at the same time share the W tiles in L2 and their H rows stay there.
+// The forward cuts the vocabulary into plan[2] runs, the gradient into single tiles.
+template <bool kRuns>
+struct CeWalk {
+  int pairs, nsplit, units, u, step, vt, vt1, row0, run, group, vt_begin, vt_count;
+  bool fresh;
+  __device__ __forceinline__ CeWalk(const CeTileParams& p, int pair, int num_pairs) {
+    pairs = p.plan[1];
+    nsplit = kRuns ? p.plan[2] : p.vt_count;
+    units = pairs * nsplit;
+    u = pair - num_pairs;
+    step = num_pairs;
+    vt = vt1 = row0 = run = 0;
+    group = p.group_pairs;
+    vt_begin = p.vt_begin;
+    vt_count = p.vt_count;
+    fresh = false;
+  }
+  __device__ __forceinline__ bool next(PairTile& t) {
+    if (vt >= vt1) {
+      u += step;
+      if (u >= units) return false;
+      const int per_group = group * nsplit;
+      const int gi = u / per_group, local = u - gi * per_group;
+      const int gsize = min(group, pairs - gi * group);
+      run = local / gsize;
+      row0 = 256 * (gi * group + local % gsize);
+      vt = vt_begin + static_cast<int>(static_cast<long long>(vt_count) * run / nsplit);
+      vt1 = vt_begin + static_cast<int>(static_cast<long long>(vt_count) * (run + 1) / nsplit);
+      fresh = true;
+    }
+    t.row0 = row0;
+    t.tile = vt++;
+    t.run = run;
+    t.first = fresh;
+    t.last = vt >= vt1;
+    fresh = false;
+    return true;
+  }
+};
+
+// Forward: running maximum and sum of the scaled logits of this thread's row over a run of tiles.
+struct CeForwardEpi {
+  using Params = CeTileParams;
+  using Walk = CeWalk<true>;
+  static constexpr int kOuts = 0;
+  static constexpr bool kF32 = false;
+  static __device__ __forceinline__ int steps(const Params&, const PairTile&, int, int) { return 4; }
+  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int, int, int) { return false; }
+  static __device__ __forceinline__ int out_col(const Params&, const PairTile&) { return 0; }
+  const Params& p;
+  int pair_row, half, row, y, tc;
+  float m, s;
+  __device__ __forceinline__ CeForwardEpi(const Params& p_, int pair_row_, int half_)
+      : p(p_), pair_row(pair_row_), half(half_), row(0), y(-1), tc(p_.plan[3]), m(-INFINITY), s(0.f) {}
+  __device__ __forceinline__ void begin(const PairTile& t) {
+    if (!t.first) return;
+    row = t.row0 + pair_row;
+    y = row < tc ? p.cy[row] : -1;
+    m = -INFINITY;
+    s = 0.f;
+  }
+  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0, uint32_t (&)[1][16]) {
+    const int nvalid = p.V - col0;
+    if (nvalid <= 0) return;
+    float z[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) z[i] = __uint_as_float(acc[i]) * p.scale2;
+    if (nvalid < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i >= nvalid) z[i] = -INFINITY;
+    }
+    const int yi = y - col0;
+    if (static_cast<unsigned>(yi) < 32u) {  // the label is one of these columns (once per row)
+      float zy = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) zy = i == yi ? z[i] : zy;
+      p.zlabel[row] = zy;
+    }
+    float c[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+    for (int i = 4; i < 32; ++i) c[i & 3] = fmaxf(c[i & 3], z[i]);
+    const float top = fmaxf(fmaxf(c[0], c[1]), fmaxf(c[2], c[3]));
+    if (top > m) {
+      s *= ex2f(m - top);
+      m = top;
+    }
+    // a row of -inf so far (or of NaN): subtracting it from itself would make NaN out of -inf
+    const float base = m == -INFINITY ? 0.f : m;
+    float a[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 32; ++i) a[i & 3] += ex2f(z[i] - base);
+    s += (a[0] + a[1]) + (a[2] + a[3]);
+  }
+  __device__ __forceinline__ void end(const PairTile& t) {
+    if (t.last && row < tc) p.partials[static_cast<size_t>(2 * t.run + half) * p.rows + row] = make_float2(m, s);
+  }
+};
+
+// Gradient: G = w (p - [c = y]) in bf16 into the scratch block of this piece of the vocabulary.
+struct CeGradientEpi {
+  using Params = CeTileParams;
+  using Walk = CeWalk<false>;
+  static constexpr int kOuts = 1;
+  static constexpr bool kF32 = false;
+  static __device__ __forceinline__ int steps(const Params& p, const PairTile&, int, int row0) {
+    return row0 < 128 * p.plan[0] ? 4 : 0;  // a CTA whose block of rows does not exist stores nothing
+  }
+  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int, int, int) { return true; }
+  static __device__ __forceinline__ int out_col(const Params& p, const PairTile& t) { return t.tile * pair_cfg::BN - p.g_col0; }
+  const Params& p;
+  int pair_row, tc, y, row0;
+  float w, lse2;
+  __device__ __forceinline__ CeGradientEpi(const Params& p_, int pair_row_, int)
+      : p(p_), pair_row(pair_row_), tc(p_.plan[3]), y(-1), row0(-1), w(0.f), lse2(1e30f) {}
+  __device__ __forceinline__ void begin(const PairTile& t) {
+    if (t.row0 == row0) return;
+    row0 = t.row0;
+    const int row = row0 + pair_row;
+    const bool on = row < tc;
+    y = on ? p.cy[row] : -1;
+    w = on ? p.cw[row] : 0.f;
+    lse2 = on ? p.lse2[row] : 1e30f;  // beyond the last row: p = 0, G = 0
+  }
+  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0, uint32_t (&out)[1][16]) {
+    float g[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) g[i] = w * ex2f(fmaf(__uint_as_float(acc[i]), p.scale2, -lse2));
+    const int yi = y - col0;
+    if (static_cast<unsigned>(yi) < 32u) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i == yi) g[i] = w * (ex2f(fmaf(__uint_as_float(acc[i]), p.scale2, -lse2)) - 1.f);
+    }
+    const int nvalid = p.V - col0;
+    if (nvalid < 32) {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (i >= nvalid) g[i] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) out[0][i] = pack_bf16x2(g[2 * i], g[2 * i + 1]);
+  }
+  __device__ __forceinline__ void end(const PairTile&) {}
+};
+
+struct CeMergeParams {
+  int T;
+  const int* plan;
+  const int* cidx;
+  const float2* partials;
+  long long rows;
+  const float* zlabel;  // the label's scaled logit as the tiles have it
+  const float* zy;      // and as the fp32 dot product has it
+  float* nll;
+  float* lse;   // or NULL
+  float* lse2;  // [rows] for the gradient tiles
+};
+
+// Merges the runs' maxima and sums into a token's log-sum-exp.
+// The tensor core cuts its partial sums instead of rounding them, so a logit is off by about 1e-6 of its
+// size in one direction.  In the sum over a vocabulary that averages out; the label's logit stands alone.  It
+// is therefore taken again as an fp32 dot product, and the difference e (that of the label's logit to
+// the tiles' value) enters to first order: lse + p e, nll - (1 - p) e, p the label's probability.  e is
+// around 1e-5, so the second order is below fp32.  (Subtracting an exact logit from an inexact lse
+// instead would spoil the losses near 0, where the two are nearly equal.)  A block takes 32 tokens (one per lane,
+// so that neighbouring compact rows are read together) and spreads the runs over its 8 warps.
+__global__ void __launch_bounds__(256) ce_merge_kernel(const CeMergeParams p) {
+  __shared__ float sm[8][32], ss[8][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x * 32 + lane;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int c = t < p.T ? p.cidx[t] : -1;
+  const int slots = 2 * p.plan[2];
+  float m = -INFINITY, s = 0.f;
+  if (c >= 0) {
+    for (int i = warp; i < slots; i += 8) {
+      const float2 q = p.partials[static_cast<size_t>(i) * p.rows + c];
+      const float top = fmaxf(m, q.x), base = top == -INFINITY ? 0.f : top;
+      s = s * ex2f(m - base) + q.y * ex2f(q.x - base);
+      m = top;
+    }
+  }
+  sm[warp][lane] = m;
+  ss[warp][lane] = s;
+  __syncthreads();
+  if (warp != 0 || t >= p.T) return;
+  float top = sm[0][lane];
+#pragma unroll
+  for (int w = 1; w < 8; ++w) top = fmaxf(top, sm[w][lane]);
+  const float base = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) sum = fmaf(ss[w][lane], ex2f(sm[w][lane] - base), sum);
+  float nll = 0.f, lse = 0.f;
+  if (c >= 0) {
+    const float l2 = base + log2f(sum), zl = p.zlabel[c];
+    const float e = p.zy[c] - zl, prob = ex2f(zl - l2);
+    p.lse2[c] = l2;
+    lse = kLn2 * fmaf(prob, e, l2);
+    nll = kLn2 * fmaf(prob - 1.f, e, l2 - zl);
+    nll = nll < 0.f ? 0.f : nll;  // rounding may dip below 0; NaN stays NaN
+  }
+  p.nll[t] = nll;
+  if (p.lse != nullptr) p.lse[t] = lse;
+}
+
+// fp32 dH sums over the compact rows, times `scale` -> bf16 rows of the tokens; tokens that do not count
+// get zeros.  8 elements per thread.
+__global__ void __launch_bounds__(256) ce_scatter_kernel(const float* __restrict__ src, const int* __restrict__ cidx,
+                                                        int T, int d, float scale, __nv_bfloat16* dst, long long ld) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
+  const int per_row = d / 8;
+  if (i >= static_cast<long long>(T) * per_row) return;
+  const int t = static_cast<int>(i / per_row), k = static_cast<int>(i % per_row) * 8;
+  const int c = cidx[t];
+  uint4 o = make_uint4(0u, 0u, 0u, 0u);
+  if (c >= 0) {
+    const float4 a = *reinterpret_cast<const float4*>(src + static_cast<size_t>(c) * d + k);
+    const float4 b = *reinterpret_cast<const float4*>(src + static_cast<size_t>(c) * d + k + 4);
+    o.x = pack_bf16x2(scale * a.x, scale * a.y);
+    o.y = pack_bf16x2(scale * a.z, scale * a.w);
+    o.z = pack_bf16x2(scale * b.x, scale * b.y);
+    o.w = pack_bf16x2(scale * b.z, scale * b.w);
+  }
+  *reinterpret_cast<uint4*>(dst + static_cast<size_t>(t) * ld + k) = o;
+}
+
+}  // namespace npd

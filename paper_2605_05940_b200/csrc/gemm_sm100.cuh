@@ -2,7 +2,7 @@
 // backward contractions of the LM head (dH = dO_S W and dW = dO_S^T H, the
 // chain rule through Algorithm 1's student-logit step).
 //
-//   D[M,N] (+)= sum_k A[m,k] * B[n,k]
+//   D[M,N] (+)= alpha sum_k A[m,k] * B[n,k]
 //
 // Either operand may be "K-major" (memory [rows][K contiguous]) or "MN-major"
 // (memory [K][rows contiguous]); the second form lets the logit-gradient block
@@ -51,6 +51,7 @@ struct GemmProblem {
   int k_splits;    // > 1 only with out_reduce
   int out_f32;     // output elements: 1 = fp32, 0 = bf16
   int out_reduce;  // 1 = D += acc (atomic, any number of adders), 0 = D = acc
+  float alpha = 1.f;  // the accumulator is multiplied by it first, in fp32
   // Extents only known on the device (the backward runs over the compact rows of a packed
   // batch, nblocks[0] blocks of 128):
   int dyn_m;       // M = 128 * nblocks[0]
@@ -481,13 +482,15 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
           } else if (g.out_f32) {
             tmem_ld16(taddr + j * 16, w);
             tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 16; ++q) w[q] = __float_as_uint(g.alpha * __uint_as_float(w[q]));
           } else {
             uint32_t r0[32];
             tmem_ld32(taddr + j * 32, r0);
             tmem_ld_wait();
 #pragma unroll
             for (int q = 0; q < 16; ++q)
-              w[q] = pack_bf16x2(__uint_as_float(r0[2 * q]), __uint_as_float(r0[2 * q + 1]));
+              w[q] = pack_bf16x2(g.alpha * __uint_as_float(r0[2 * q]), g.alpha * __uint_as_float(r0[2 * q + 1]));
           }
           if (j == nsteps - 1) {
             // everything this warp needs from tensor memory is in registers: release the accumulators

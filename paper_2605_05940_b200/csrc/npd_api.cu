@@ -273,7 +273,8 @@ int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const
   GemmParams gp{};
   long long units = 0;
   for (int i = 0; i < 2; ++i) {
-    const int j = i < nprob ? i : 0;  // an unused slot repeats problem 0's (valid) maps
+    int j = i < nprob ? i : 0;        // an unused slot repeats problem 0's (valid) maps
+    if (pr[j].M == 0 && !pr[j].dyn_m) j = 1;  // a problem without rows has no maps of its own
     const GemmProblem& g = pr[j];
     // extents as the maps see them: device-side dimensions take their upper bound
     const uint64_t am = g.dyn_m ? 128ull * max_blocks : g.M, ak = g.dyn_k ? 128ull * max_blocks : g.K;
@@ -286,8 +287,8 @@ int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const
     const bool oko = make_map(&maps[3 * i + 2], ops[j].out, g.N, om, ops[j].ldo, g.out_f32 ? 16 : 32, BM,
                               g.out_f32 != 0, true, true);
     if (!oka || !okb || !oko) return NPD_ECUDA;
-    gp.pr[i] = g;
-    if (i < nprob)
+    gp.pr[i] = pr[i < nprob ? i : 0];
+    if (i < nprob && j == i)
       units += static_cast<long long>((am + PM - 1) / PM) * ((g.N + BN - 1) / BN) * g.k_splits;
   }
   gp.nprob = nprob;
@@ -940,3 +941,4 @@ int npd_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, i
 }  // extern "C"
 
 #include "norm_api.cuh"
+#include "ce_api.cuh"
