@@ -470,6 +470,66 @@ typedef struct npd_ce_args {
 int npd_ce_workspace_bytes(const npd_ce_args* args, size_t* out_bytes);
 int npd_ce_fwd_bwd(const npd_ce_args* args, void* cuda_stream);
 
+/* activation of npd_linear_args */
+enum {
+  NPD_ACT_NONE = 0,
+  NPD_ACT_RELU = 1,
+  NPD_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function */
+  NPD_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+  NPD_ACT_SILU = 4       /* z / (1 + e^-z) */
+};
+
+/* flags of npd_linear_args */
+enum { NPD_LINEAR_ACCUMULATE_DW = 1 /* add into dw instead of overwriting it (f32 dw only) */ };
+
+/*
+ * A linear layer with bias, activation and residual in the epilogue of the product, and its backward
+ * (npd_gemm_bf16 is the plain product):
+ *
+ *   z[m,n] = sum_k x[m,k] weight[n,k] + bias[n]
+ *   y[m,n] = act(z[m,n]) + residual[m,n]
+ *   dz = dy act'(z),  dx = dz weight,  dw = dz^T x,  dbias = sum_m dz          (the residual's gradient is dy)
+ *
+ * x, weight, preact and dy are bf16, y and residual both of `y_dtype`, bias of `bias_dtype`, dbias f32.  z
+ * stays in fp32 up to y, which is rounded once; with preact given z is stored too, rounded to bf16, for the
+ * backward, which takes it in its place (not needed for NPD_ACT_NONE).  dz is rounded to bf16 on its way to dx
+ * and dw (dbias sums the unrounded values), so an fp32 dw has fp32 sums of bf16-rounded terms.
+ *
+ * Row-major, row strides in ELEMENTS, matrices on 16-byte boundaries with row strides that are multiples of 16
+ * bytes; any M, N, K >= 1.  bias needs no alignment beyond its type's.  y may be residual itself (same pointer and
+ * stride); any other overlap of a result with an operand or another result is refused (NPD_EINVAL).
+ *
+ * Every result is bitwise reproducible, but for a dw that is added to (atomic adds, one per element and call).
+ * `status` (int32[1], may be NULL) receives NPD_ETIMEOUT if a bounded wait ran out in the forward, else it is left
+ * untouched.  The backward keeps its status word in the workspace (npd_last_status): npd_linear_workspace_bytes,
+ * 1024-byte aligned, one call at a time.
+ */
+typedef struct npd_linear_args {
+  size_t size;               /* = sizeof(npd_linear_args); checked */
+  int32_t M, N, K, activation;
+  int32_t bias_dtype, y_dtype, dw_dtype, flags;
+  const void* x;             /* bf16 [M, ldx]  (backward: needed for dw) */
+  const void* weight;        /* bf16 [N, ldw]  */
+  const void* bias;          /* [N] or NULL    */
+  const void* residual;      /* [M, ldr] or NULL */
+  void* y;                   /* [M, ldy]       */
+  void* preact;              /* bf16 [M, ldz] or NULL; output of the forward, input of the backward */
+  int64_t ldx, ldw, ldr, ldy, ldz;
+  const void* dy;            /* bf16 [M, lddy] */
+  void* dx;                  /* bf16 [M, lddx] or NULL */
+  void* dw;                  /* [N, lddw] or NULL */
+  float* dbias;              /* [N] or NULL    */
+  int64_t lddy, lddx, lddw;
+  int32_t* status;
+  void* workspace;
+  size_t workspace_bytes;
+} npd_linear_args;
+
+int npd_linear_fwd(const npd_linear_args* args, void* cuda_stream);
+int npd_linear_bwd(const npd_linear_args* args, void* cuda_stream);
+/* HOST.  Bytes of workspace npd_linear_bwd needs (pointers inside args are not read). */
+int npd_linear_workspace_bytes(const npd_linear_args* args, size_t* out_bytes);
+
 /* flags of npd_norm_args */
 enum { NPD_NORM_POST = 1 /* the branch goes through a norm of its own before it is added */ };
 

@@ -618,3 +618,43 @@ def norm_join_backward(dy, h, x, dh=None, gate=None, post_weight=None, pre_weigh
     out["d_post_weight"] = np.sum(dn * unit, axis=0)
     out["dx"] = _rms_norm_backward(dn * gain, x, eps) if post_norm else dn
     return out
+
+
+def activation(z, name):
+    """Value and derivative of an activation: none, relu, gelu (normal distribution function), gelu_tanh
+    (its tanh form), silu."""
+    z = np.asarray(z, np.float64)
+    with np.errstate(over="ignore"):
+        if name == "none":
+            return z, np.ones_like(z)
+        if name == "relu":
+            return np.where(z < 0, 0.0, z), (z > 0).astype(np.float64)
+        if name == "silu":
+            q = 1.0 / (1.0 + np.exp(-z))
+            return z * q, q * (1.0 + z * (1.0 - q))
+        if name == "gelu":
+            from math import erfc
+            cdf = 0.5 * np.vectorize(erfc, otypes=[np.float64])(-z / np.sqrt(2.0))
+            return z * cdf, cdf + z * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)
+        if name == "gelu_tanh":
+            k = np.sqrt(2.0 / np.pi)
+            t = np.tanh(k * (z + 0.044715 * z ** 3))
+            return 0.5 * z * (1.0 + t), 0.5 * (1.0 + t) + 0.5 * z * (1.0 - t * t) * k * (1.0 + 3 * 0.044715 * z * z)
+    raise ValueError(name)
+
+
+def linear(x, w, bias=None, residual=None, act="none"):
+    """(y, z) of z = x w^T + bias, y = act(z) + residual."""
+    z = np.asarray(x, np.float64) @ np.asarray(w, np.float64).T
+    if bias is not None:
+        z = z + np.asarray(bias, np.float64)
+    y = activation(z, act)[0]
+    return (y if residual is None else y + np.asarray(residual, np.float64)), z
+
+
+def linear_backward(dy, x, w, z=None, act="none"):
+    """(dx, dw, dbias, dz) from dy; z is the pre-activation the forward kept."""
+    dz = np.asarray(dy, np.float64)
+    if act != "none":
+        dz = dz * activation(z, act)[1]
+    return dz @ np.asarray(w, np.float64), dz.T @ np.asarray(x, np.float64), dz.sum(axis=0), dz

@@ -30,6 +30,8 @@ NPD_SELECT_TEACHER_IFD_LE_1 = 1
 NPD_SELECT_SCORE_IFD_TEACHER, NPD_SELECT_SCORE_IFD_STUDENT = 2, 4
 NPD_SELECT_LO_EXCLUSIVE, NPD_SELECT_HI_EXCLUSIVE = 8, 16
 NPD_NORM_POST = 1
+NPD_LINEAR_ACCUMULATE_DW = 1
+NPD_ACT_NONE, NPD_ACT_RELU, NPD_ACT_GELU, NPD_ACT_GELU_TANH, NPD_ACT_SILU = range(5)
 NPD_CE_ACCUMULATE_DW, NPD_CE_SERIALIZE_LAUNCHES = 1, 2
 NPD_GEMM_STORE_F32, NPD_GEMM_ADD_F32, NPD_GEMM_STORE_BF16, NPD_GEMM_ATOMIC_F32 = range(4)
 
@@ -38,7 +40,7 @@ EXPORTS = ("npd_workspace_bytes", "npd_phase_count", "npd_kd_fwd_bwd", "npd_kd_f
            "npd_kd_forward_noalloc", "npd_pack_sequences", "npd_last_copy_bytes",
            "npd_kd_fwd_bwd_host_streams", "npd_perplexity", "npd_selftest_wait_timeout",
            "npd_debug_chunk_schedule", "npd_norm_fwd", "npd_norm_bwd", "npd_norm_workspace_bytes",
-           "npd_ce_fwd_bwd", "npd_ce_workspace_bytes")
+           "npd_ce_fwd_bwd", "npd_ce_workspace_bytes", "npd_linear_fwd", "npd_linear_bwd", "npd_linear_workspace_bytes")
 NPD_STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
 
@@ -95,6 +97,19 @@ class npd_ce_args(C.Structure):
     ]
 
 
+class npd_linear_args(C.Structure):
+    _fields_ = [
+        ("size", C.c_size_t), ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("activation", C.c_int32),
+        ("bias_dtype", C.c_int32), ("y_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("flags", C.c_int32),
+        ("x", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p), ("residual", C.c_void_p), ("y", C.c_void_p),
+        ("preact", C.c_void_p),
+        ("ldx", C.c_int64), ("ldw", C.c_int64), ("ldr", C.c_int64), ("ldy", C.c_int64), ("ldz", C.c_int64),
+        ("dy", C.c_void_p), ("dx", C.c_void_p), ("dw", C.c_void_p), ("dbias", C.c_void_p),
+        ("lddy", C.c_int64), ("lddx", C.c_int64), ("lddw", C.c_int64),
+        ("status", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
 _lib = None
 
 
@@ -135,6 +150,9 @@ def lib() -> C.CDLL:
         for f in (l.npd_norm_fwd, l.npd_norm_bwd):
             f.argtypes = [C.POINTER(npd_norm_args), C.c_void_p]
         l.npd_norm_workspace_bytes.argtypes = [C.POINTER(npd_norm_args), C.POINTER(C.c_size_t)]
+        for f in (l.npd_linear_fwd, l.npd_linear_bwd):
+            f.argtypes = [C.POINTER(npd_linear_args), C.c_void_p]
+        l.npd_linear_workspace_bytes.argtypes = [C.POINTER(npd_linear_args), C.POINTER(C.c_size_t)]
         l.npd_ce_fwd_bwd.argtypes = [C.POINTER(npd_ce_args), C.c_void_p]
         l.npd_ce_workspace_bytes.argtypes = [C.POINTER(npd_ce_args), C.POINTER(C.c_size_t)]
         _lib = l
@@ -541,6 +559,88 @@ def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_wei
                 a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         _check(lib().npd_norm_bwd(a, _current(dev)), where)
     return dx, dresidual, d_post, d_pre, d_gate
+
+
+def npd_linear_fwd(x, weight, *, bias=None, activation=NPD_ACT_NONE, residual=None, want_preact=False,
+                   y_dtype=torch.bfloat16, y=None, preact=None, status=None, stream=None):
+    """y = act(x weight^T + bias) + residual (see npd_linear_args in include/npd.h).  x bf16 [M, K], weight bf16
+    [N, K], bias bf16 or f32 [N], residual of y's type [M, N].  Results go to y and preact or to new tensors
+    (want_preact: the bf16 pre-activation that the backward needs); returns (y, preact)."""
+    where = "npd_linear_fwd"
+    dev = _device_of(x, where)
+    if x.dim() != 2 or weight.dim() != 2:
+        raise NpdError(NPD_ESHAPE, where)
+    (M, K), N, bf16 = x.shape, weight.shape[0], torch.bfloat16
+    if y is not None:
+        y_dtype = y.dtype
+    elif residual is not None:
+        y_dtype = residual.dtype
+    if y_dtype not in _DT or (bias is not None and bias.dtype not in _DT):
+        raise NpdError(NPD_EINVAL, where)
+    with _scope(dev, stream):
+        a = npd_linear_args(C.sizeof(npd_linear_args), M, N, K, activation, 0 if bias is None else _DT[bias.dtype],
+                            _DT[y_dtype])
+        a.ldx, a.x = _matrix(x, where, dev, (M, K), bf16), x.data_ptr()
+        a.ldw, a.weight = _matrix(weight, where, dev, (N, K), bf16), weight.data_ptr()
+        if bias is not None:
+            a.bias = _vector(bias, where, dev, N, bias.dtype)
+        if residual is not None:
+            a.ldr, a.residual = _matrix(residual, where, dev, (M, N), y_dtype), residual.data_ptr()
+        if y is None:
+            y = _new((M, N), y_dtype, x.device)
+        a.ldy, a.y = _matrix(y, where, dev, (M, N), y_dtype), y.data_ptr()
+        if preact is None and want_preact:
+            preact = _new((M, N), bf16, x.device)
+        if preact is not None:
+            a.ldz, a.preact = _matrix(preact, where, dev, (M, N), bf16), preact.data_ptr()
+        if status is not None:
+            a.status = _vector(status, where, dev, 1, torch.int32)
+        _check(lib().npd_linear_fwd(a, _current(dev)), where)
+    return y, preact
+
+
+def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_dx=True, want_dw=True, want_dbias=False,
+                   dw_dtype=torch.bfloat16, dx=None, dw=None, accumulate_dw=False, workspace=None, stream=None):
+    """Gradients of npd_linear_fwd from dy bf16 [M, N]: (dx bf16 [M, K], dw [N, K], dbias f32 [N]), None for what
+    is not wanted.  preact is the forward's (not needed without an activation), x only for dw.  An f32 dw with
+    accumulate_dw is added to.  The gradient of the residual is dy itself."""
+    where = "npd_linear_bwd"
+    dev = _device_of(dy, where)
+    if dy.dim() != 2 or weight is None or weight.dim() != 2:
+        raise NpdError(NPD_ESHAPE, where)
+    (M, N), K, device, bf16 = dy.shape, weight.shape[1], dy.device, torch.bfloat16
+    if dw is not None:
+        dw_dtype = dw.dtype
+    if dw_dtype not in _DT:
+        raise NpdError(NPD_EINVAL, where)
+    with _scope(dev, stream):
+        a = npd_linear_args(C.sizeof(npd_linear_args), M, N, K, activation, 0, 0, _DT[dw_dtype],
+                            NPD_LINEAR_ACCUMULATE_DW if accumulate_dw else 0)
+        a.lddy, a.dy = _matrix(dy, where, dev, (M, N), bf16), dy.data_ptr()
+        a.ldw, a.weight = _matrix(weight, where, dev, (N, K), bf16), weight.data_ptr()
+        if x is not None:
+            a.ldx, a.x = _matrix(x, where, dev, (M, K), bf16), x.data_ptr()
+        if preact is not None:
+            a.ldz, a.preact = _matrix(preact, where, dev, (M, N), bf16), preact.data_ptr()
+        if dx is None and want_dx:
+            dx = _new((M, K), bf16, device)
+        if dx is not None:
+            a.lddx, a.dx = _matrix(dx, where, dev, (M, K), bf16), dx.data_ptr()
+        if dw is None and want_dw:
+            dw = _new((N, K), dw_dtype, device)
+        if dw is not None:
+            a.lddw, a.dw = _matrix(dw, where, dev, (N, K), dw_dtype), dw.data_ptr()
+        dbias = torch.empty(N, dtype=torch.float32, device=device) if want_dbias else None
+        a.dbias = _ptr(dbias)
+        if workspace is None:
+            n = C.c_size_t(0)
+            _check(lib().npd_linear_workspace_bytes(a, n), where)
+            workspace, a.workspace = _workspace(n.value, device)
+            a.workspace_bytes = n.value
+        else:
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        _check(lib().npd_linear_bwd(a, _current(dev)), where)
+    return dx, dw, dbias
 
 
 class CEStep:

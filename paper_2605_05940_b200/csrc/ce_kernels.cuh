@@ -204,7 +204,7 @@ struct CeForwardEpi {
   static constexpr int kOuts = 0;
   static constexpr bool kF32 = false;
   static __device__ __forceinline__ int steps(const Params&, const PairTile&, int, int) { return 4; }
-  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int, int, int) { return false; }
+  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int) { return false; }
   static __device__ __forceinline__ int out_col(const Params&, const PairTile&) { return 0; }
   const Params& p;
   int pair_row, half, row, y, tc;
@@ -265,7 +265,7 @@ struct CeGradientEpi {
   static __device__ __forceinline__ int steps(const Params& p, const PairTile&, int, int row0) {
     return row0 < 128 * p.plan[0] ? 4 : 0;  // a CTA whose block of rows does not exist stores nothing
   }
-  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int, int, int) { return true; }
+  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int) { return true; }
   static __device__ __forceinline__ int out_col(const Params& p, const PairTile& t) { return t.tile * pair_cfg::BN - p.g_col0; }
   const Params& p;
   int pair_row, tc, y, row0;

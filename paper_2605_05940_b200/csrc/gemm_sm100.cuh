@@ -58,6 +58,11 @@ struct GemmProblem {
   int dyn_k;       // K = 128 * nblocks[0]
   int stream_k;    // problem 1 only: cut along the (tile, k-step) line as described above
                    // (needs out_reduce and k_splits = 1)
+  // A TMA store clips the matrix's last column to a 16-byte boundary, not to the element.  With N beyond such a
+  // boundary (`ragged`) the sub-tile across the edge is written by the epilogue threads themselves.
+  int ragged;
+  void* out;
+  long long ldo;
 };
 
 struct GemmParams {
@@ -243,6 +248,22 @@ struct GemmWalk {
     return true;
   }
 };
+
+// Writes the elements inside N (`n` of them) of one row of the sub-tile across the matrix's last column.
+__device__ __forceinline__ void gemm_store_edge(void* out, size_t at, int n, bool f32, bool add, const uint32_t (&w)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (f32) {
+      float* o = static_cast<float*>(out) + at + i;
+      if (i < n && add) atomicAdd(o, __uint_as_float(w[i]));
+      else if (i < n) *o = __uint_as_float(w[i]);
+    } else {
+      uint16_t* o = static_cast<uint16_t*>(out) + at + 2 * i;
+      if (2 * i < n) o[0] = static_cast<uint16_t>(w[i]);
+      if (2 * i + 1 < n) o[1] = static_cast<uint16_t>(w[i] >> 16);
+    }
+  }
+}
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_cfg::THREADS, 1)
 gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_constant__ CUtensorMap tmap_b0,
@@ -439,7 +460,9 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
             if (!(ok = mbar_wait(ofull0 + 8 * b, (oit / OUT_BUFS) & 1, abort_flag))) break;
             const uint32_t src = smem_u32(smem + OFF_OUT + b * OUT_BYTES);
             const int col = u.n0 + c0 + j * step;
-            if (g.out_reduce)
+            if (g.ragged && col + step > g.N) {
+              // written by the epilogue threads
+            } else if (g.out_reduce)
               tma_reduce_add_2d(to, src, col, row0);
             else
               tma_store_2d(to, src, col, row0);
@@ -501,6 +524,12 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
           const int b = grp * OUT_BUFS + static_cast<int>(oit % OUT_BUFS);
           ok = __all_sync(0xffffffffu, mbar_wait(oempty0 + 8 * b, ((oit / OUT_BUFS) & 1) ^ 1, abort_flag));
           if (!ok) break;
+          const int col = u.n0 + c0 + j * step;
+          if (g.ragged && col + step > g.N) {
+            const int row = u.m0 + static_cast<int>(rank) * BM + row_local;
+            if (row < g.M)
+              gemm_store_edge(g.out, static_cast<size_t>(row) * g.ldo + col, g.N - col, g.out_f32 != 0, g.out_reduce != 0, w);
+          }
           uint8_t* orow = smem + OFF_OUT + b * OUT_BYTES + row_local * 64;
 #pragma unroll
           for (int q = 0; q < 4; ++q)

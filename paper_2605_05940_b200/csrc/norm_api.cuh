@@ -231,18 +231,8 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   if (e != cudaSuccess) return NPD_ECUDA;
   if (p.want != 0) {
     float* shared_dgate = (p.want & 4) ? static_cast<float*>(a->d_gate) : nullptr;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>((a->d + 31) / 32), 3);
-    cfg.blockDim = dim3(512);
-    cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, column_sum_kernel, static_cast<const float*>(p.part), pl.grid,
-                           3ll * a->d, static_cast<long long>(a->d), a->d, a->d_pre_weight, a->d_post_weight,
-                           shared_dgate);
+    e = launch_dim(column_sum_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 3), 512, 0, st, true, p.part, pl.grid,
+                   3ll * a->d, a->d, a->d, a->d_pre_weight, a->d_post_weight, shared_dgate);
     ++g_launches;
   }
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;

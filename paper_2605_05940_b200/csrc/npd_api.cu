@@ -14,7 +14,9 @@
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
+#include <utility>
 #include <vector>
 
 #include "gemm_sm100.cuh"
@@ -214,10 +216,10 @@ int set_smem(K kernel, int bytes) {
 // of this kernel may be scheduled and run their prologue while the kernel before it in the stream
 // is still draining; they wait for that kernel's completion inside (griddepcontrol.wait).
 template <typename... P, typename... A>
-cudaError_t launch_ex(void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t st, bool pdl,
-                      A&&... args) {
+cudaError_t launch_dim(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t st, bool pdl,
+                       A&&... args) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.dynamicSmemBytes = static_cast<size_t>(smem);
   cfg.stream = st;
@@ -227,6 +229,11 @@ cudaError_t launch_ex(void (*kernel)(P...), int grid, int threads, int smem, cud
   cfg.attrs = at;
   cfg.numAttrs = pdl ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t launch_ex(void (*kernel)(P...), int grid, int threads, int smem, cudaStream_t st, bool pdl,
+                      A&&... args) {
+  return launch_dim(kernel, dim3(static_cast<unsigned>(grid)), threads, smem, st, pdl, std::forward<A>(args)...);
 }
 
 struct GemmOperands {
@@ -288,6 +295,9 @@ int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const
                               g.out_f32 != 0, true, true);
     if (!oka || !okb || !oko) return NPD_ECUDA;
     gp.pr[i] = pr[i < nprob ? i : 0];
+    gp.pr[i].out = ops[j].out;
+    gp.pr[i].ldo = ops[j].ldo;
+    gp.pr[i].ragged = (g.N * (g.out_f32 ? 4 : 2)) % 16 != 0;
     if (i < nprob && j == i)
       units += static_cast<long long>((am + PM - 1) / PM) * ((g.N + BN - 1) / BN) * g.k_splits;
   }
@@ -942,3 +952,4 @@ int npd_gemm_bf16(int32_t M, int32_t N, int32_t K, const void* A, int64_t lda, i
 
 #include "norm_api.cuh"
 #include "ce_api.cuh"
+#include "linear_api.cuh"

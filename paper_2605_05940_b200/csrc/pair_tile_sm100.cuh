@@ -24,10 +24,14 @@
 // Epi provides (all evaluated by every role alike unless said otherwise):
 //   Params                     launch parameters, with `int* status` and `int ksteps`
 //   Walk(p, pair, pairs, rank) the tiles of a pair: bool next(PairTile&)
-//   kOuts                      tile-sized results per tile (0, 1 or 2); kF32 = they are fp32, else bf16
+//   kOuts                      tile-sized results per tile (0, 1 or 2); kF32 = the first is fp32, else bf16
+//                              (a second one is always bf16)
 //   steps(p, tile, half, row0) 32-column chunks of this half that have to be stored (0 .. 4)
+//   keeps(p, tile, col)        whether a staging buffer whose first column is `col` of the tile is stored
+//   out_col(p, tile)           column of the results that the tile's column 0 goes to
 //   Epi(p, row_local, half)    per epilogue thread; then for every tile begin(tile), for every chunk
-//                              chunk(acc[32], col0, out), and end(tile)
+//                              chunk(acc[32], col0, out), and end(tile); out[i] is the i-th staging buffer's
+//                              64 bytes of this row: the first result's one (bf16) or two (fp32), then the second's
 #pragma once
 
 #include "ptx_sm100.cuh"
@@ -66,8 +70,8 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
                  const typename Epi::Params p) {
   using namespace pair_cfg;
   constexpr int kOuts = Epi::kOuts;
-  constexpr int kWords = Epi::kF32 ? 32 : 16;  // 32-bit words of one chunk of one result
-  constexpr int kSub = kWords / 16;            // staging buffers one chunk of one result takes
+  constexpr int kSub = Epi::kF32 ? 2 : 1;                                     // staging buffers per chunk: first result,
+  constexpr int kPer = kOuts == 0 ? 1 : kSub + (kOuts > 1 ? 1 : 0);          // all results
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -203,14 +207,14 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       while (ok && walk.next(t)) {
         const int row0 = t.row0 + static_cast<int>(rank) * BM;
         const int n = Epi::steps(p, t, half, row0);
-        for (int j = 0; j < n * kOuts * kSub && ok; ++j, ++oit) {
+        for (int j = 0; j < n * kPer && ok; ++j, ++oit) {
           const int b = half * OUT_BUFS + static_cast<int>(oit % OUT_BUFS);
           if (!(ok = mbar_wait(ofull0 + 8 * b, (oit / OUT_BUFS) & 1, abort_flag))) break;
-          constexpr int kPer = kOuts > 0 ? kOuts * kSub : 1;  // buffers per chunk
-          const int c = j / kPer, which = j % kPer / kSub, sub = j % kSub;
-          const int col = Epi::out_col(p, t) + half * BNH + c * 32 + sub * 16;
-          if (Epi::keeps(p, t, half, c, sub))
-            tma_store_2d(which == 0 ? &tmap_o0 : &tmap_o1, smem_u32(smem + OFF_OUT + b * OUT_BYTES), col, row0);
+          const int c = j / kPer, which = j % kPer < kSub ? 0 : 1, sub = which == 0 ? j % kPer : 0;
+          const int col = half * BNH + c * 32 + sub * 16;  // within the tile
+          if (Epi::keeps(p, t, col))
+            tma_store_2d(which == 0 ? &tmap_o0 : &tmap_o1, smem_u32(smem + OFF_OUT + b * OUT_BYTES),
+                         Epi::out_col(p, t) + col, row0);
           tma_store_commit();
           if (prev >= 0) {
             tma_store_wait_read<1>();  // the copy before this one has read its buffer
@@ -255,15 +259,15 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         tmem_ld32(taddr + c * 32, acc);
         tmem_ld_wait();
         if (c == n - 1) release();
-        uint32_t out[kOuts > 0 ? kOuts : 1][kWords];
+        uint32_t out[kPer][16];
         epi.chunk(acc, t.tile * BN + half * BNH + c * 32, out);
         if (kOuts > 0) {
 #pragma unroll
-          for (int s = 0; s < kOuts * kSub; ++s, ++oit) {
+          for (int s = 0; s < kPer; ++s, ++oit) {
             const int b = half * OUT_BUFS + static_cast<int>(oit % OUT_BUFS);
             if (!(ok = __all_sync(0xffffffffu, mbar_wait(oempty0 + 8 * b, ((oit / OUT_BUFS) & 1) ^ 1, abort_flag)))) break;
             uint8_t* orow = smem + OFF_OUT + b * OUT_BYTES + row_local * 64;
-            const uint32_t* w = &out[s / kSub][(s % kSub) * 16];
+            const uint32_t* w = out[s];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
               *reinterpret_cast<uint4*>(orow + ((static_cast<uint32_t>(q) ^ swz) << 4)) =

@@ -76,3 +76,21 @@ def test_norm_join_matches_torch_and_differences(post_norm, gate, offset):
     if g is not None:
         dg = got["d_gate"] if gate == "token" else got["d_gate"].sum(0)
         assert np.allclose(dg, _diff(loss, g), atol=1e-7)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+def test_linear_matches_torch_and_differences(act):
+    rng = np.random.default_rng(6)
+    M, N, K = 4, 3, 5
+    x, w, b, r = rng.normal(size=(M, K)), rng.normal(size=(N, K)), rng.normal(size=N), rng.normal(size=(M, N))
+    f = torch.nn.functional
+    fn = {"none": lambda v: v, "relu": torch.relu, "gelu": f.gelu, "gelu_tanh": lambda v: f.gelu(v, approximate="tanh"),
+          "silu": f.silu}[act]
+    y, z = orc.linear(x, w, b, r, act)
+    want = fn(torch.from_numpy(x @ w.T + b)).numpy() + r
+    assert np.allclose(y, want, rtol=1e-12, atol=1e-14)
+    c = rng.normal(size=(M, N))
+    loss = lambda: float(np.sum(c * orc.linear(x, w, b, r, act)[0]))
+    dx, dw, db, _ = orc.linear_backward(c, x, w, z, act)
+    assert np.allclose(dx, _diff(loss, x), atol=1e-7) and np.allclose(dw, _diff(loss, w), atol=1e-7)
+    assert np.allclose(db, _diff(loss, b), atol=1e-7)
