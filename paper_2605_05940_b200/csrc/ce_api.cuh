@@ -17,7 +17,7 @@ CePlan ce_plan(const npd_ce_args* a, int sms) {
   pl.vtiles = (a->V + 255) / 256;
   pl.clusters = std::max(sms / 2, 1);
   // As many runs as CTA pairs: a batch of one pair of row blocks (a few tokens to score) then still
-  // keeps every SM reading its own part of the weights.  The partials cost 16 bytes per token and run.
+  // keeps every SM reading its own part of the weights.  The partials cost 32 bytes per token and run.
   pl.nsplit_max = std::min(pl.vtiles, pl.clusters);
   pl.grads = a->d_hidden != nullptr || a->d_weight != nullptr;
   // Pieces of the vocabulary in the backward: by default the widest whose bf16 gradient block stays
@@ -44,7 +44,7 @@ CePlan ce_plan(const npd_ce_args* a, int sms) {
   pl.off_cy = take(sizeof(int) * crows);
   pl.off_cw = take(sizeof(float) * crows);
   pl.off_hc = take(2 * crows * a->d);
-  pl.off_partials = take(sizeof(float2) * 2 * pl.nsplit_max * crows);
+  pl.off_partials = take(sizeof(float2) * 4 * pl.nsplit_max * crows);
   pl.off_zlabel = take(sizeof(float) * crows);
   pl.off_zy = take(sizeof(float) * crows);
   pl.off_lse2 = take(sizeof(float) * crows);
@@ -98,12 +98,12 @@ int check_ce(const npd_ce_args* a, bool need_pointers) {
 
 // Launch of a pair-tile kernel: always one CTA pair per two SMs (at most `tiles` pairs when the host knows).
 template <class Epi>
-int launch_pair_tile(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& mo0, const CUtensorMap& mo1,
-                     const typename Epi::Params& p, int pairs, cudaStream_t st, bool pdl) {
+int launch_pair_tile(const CUtensorMap& ma, const CUtensorMap& mb, const typename Epi::Params& p, int pairs, cudaStream_t st,
+                     bool pdl) {
   using namespace pair_cfg;
   auto k = pair_tile_kernel<Epi>;
   if (set_smem(k, SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
-  const cudaError_t e = launch_ex(k, 2 * pairs, THREADS, SMEM_BYTES, st, pdl, ma, mb, mo0, mo1, p);
+  const cudaError_t e = launch_ex(k, 2 * pairs, THREADS, SMEM_BYTES, st, pdl, ma, mb, p);
   ++g_launches;
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;
 }
@@ -184,7 +184,7 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
   tp.zlabel = reinterpret_cast<float*>(ws + pl.off_zlabel);
   tp.lse2 = reinterpret_cast<float*>(ws + pl.off_lse2);
   tp.status = status;
-  if ((rc = launch_pair_tile<CeForwardEpi>(mh, mw, mh, mh, tp, pl.clusters, st, pdl)) != NPD_OK) return rc;
+  if ((rc = launch_pair_tile<CeForwardEpi>(mh, mw, tp, pl.clusters, st, pdl)) != NPD_OK) return rc;
 
   CeMergeParams mp{};
   mp.T = a->T;
@@ -209,13 +209,13 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
     const int cols = std::min(pl.chunk_cols, a->V - col0);
     if (cols <= 0) break;
     const int cols_pad = std::min(pl.chunk_cols, pl.vtiles * 256 - col0);
-    CUtensorMap mg;
-    if (!make_map(&mg, gbuf, cols_pad, crows, pl.chunk_cols, 32, 128, false, true, true)) return NPD_ECUDA;
     CeTileParams gp = tp;
     gp.vt_begin = col0 / 256;
     gp.vt_count = cols_pad / 256;
+    gp.gbuf = gbuf;
+    gp.ldg = pl.chunk_cols;
     gp.g_col0 = col0;
-    if ((rc = launch_pair_tile<CeGradientEpi>(mh, mw, mg, mg, gp, pl.clusters, st, pdl)) != NPD_OK) return rc;
+    if ((rc = launch_pair_tile<CeGradientEpi>(mh, mw, gp, pl.clusters, st, pdl)) != NPD_OK) return rc;
 
     GemmProblem pr[2] = {};
     GemmOperands ops[2] = {};

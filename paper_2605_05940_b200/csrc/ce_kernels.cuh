@@ -147,9 +147,11 @@ struct CeTileParams {
   int vt_begin, vt_count;
   float scale2;        // log2(e) / tau
   long long rows;      // stride of the partials: compact rows the workspace has room for
-  float2* partials;    // forward: [2 * runs][rows] {maximum, sum}, base 2, logits scaled by scale2
+  float2* partials;    // forward: [4 * runs][rows] {maximum, sum}, base 2, logits scaled by scale2
   float* zlabel;       // forward: [rows] the label's scaled logit
   const float* lse2;   // gradient: [rows] log2-sum-exp2 of the scaled logits
+  __nv_bfloat16* gbuf; // gradient: scratch block [rows, ldg], 1024-byte aligned, ldg a multiple of 256
+  long long ldg;
   int g_col0;          // gradient: vocabulary column of the scratch's column 0
   int* status;
 };
@@ -201,16 +203,11 @@ struct CeWalk {
 struct CeForwardEpi {
   using Params = CeTileParams;
   using Walk = CeWalk<true>;
-  static constexpr int kOuts = 0;
-  static constexpr bool kF32 = false;
-  static __device__ __forceinline__ int steps(const Params&, const PairTile&, int, int) { return 4; }
-  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int) { return false; }
-  static __device__ __forceinline__ int out_col(const Params&, const PairTile&) { return 0; }
   const Params& p;
-  int pair_row, half, row, y, tc;
+  int pair_row, quarter, row, y, tc;
   float m, s;
-  __device__ __forceinline__ CeForwardEpi(const Params& p_, int pair_row_, int half_)
-      : p(p_), pair_row(pair_row_), half(half_), row(0), y(-1), tc(p_.plan[3]), m(-INFINITY), s(0.f) {}
+  __device__ __forceinline__ CeForwardEpi(const Params& p_, int pair_row_, int quarter_)
+      : p(p_), pair_row(pair_row_), quarter(quarter_), row(0), y(-1), tc(p_.plan[3]), m(-INFINITY), s(0.f) {}
   __device__ __forceinline__ void begin(const PairTile& t) {
     if (!t.first) return;
     row = t.row0 + pair_row;
@@ -218,7 +215,7 @@ struct CeForwardEpi {
     m = -INFINITY;
     s = 0.f;
   }
-  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0, uint32_t (&)[1][16]) {
+  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0) {
     const int nvalid = p.V - col0;
     if (nvalid <= 0) return;
     float z[32];
@@ -252,7 +249,7 @@ struct CeForwardEpi {
     s += (a[0] + a[1]) + (a[2] + a[3]);
   }
   __device__ __forceinline__ void end(const PairTile& t) {
-    if (t.last && row < tc) p.partials[static_cast<size_t>(2 * t.run + half) * p.rows + row] = make_float2(m, s);
+    if (t.last && row < tc) p.partials[static_cast<size_t>(4 * t.run + quarter) * p.rows + row] = make_float2(m, s);
   }
 };
 
@@ -260,18 +257,11 @@ struct CeForwardEpi {
 struct CeGradientEpi {
   using Params = CeTileParams;
   using Walk = CeWalk<false>;
-  static constexpr int kOuts = 1;
-  static constexpr bool kF32 = false;
-  static __device__ __forceinline__ int steps(const Params& p, const PairTile&, int, int row0) {
-    return row0 < 128 * p.plan[0] ? 4 : 0;  // a CTA whose block of rows does not exist stores nothing
-  }
-  static __device__ __forceinline__ bool keeps(const Params&, const PairTile&, int) { return true; }
-  static __device__ __forceinline__ int out_col(const Params& p, const PairTile& t) { return t.tile * pair_cfg::BN - p.g_col0; }
   const Params& p;
-  int pair_row, tc, y, row0;
+  int pair_row, tc, blocks128, y, row0;
   float w, lse2;
   __device__ __forceinline__ CeGradientEpi(const Params& p_, int pair_row_, int)
-      : p(p_), pair_row(pair_row_), tc(p_.plan[3]), y(-1), row0(-1), w(0.f), lse2(1e30f) {}
+      : p(p_), pair_row(pair_row_), tc(p_.plan[3]), blocks128(128 * p_.plan[0]), y(-1), row0(-1), w(0.f), lse2(1e30f) {}
   __device__ __forceinline__ void begin(const PairTile& t) {
     if (t.row0 == row0) return;
     row0 = t.row0;
@@ -281,7 +271,8 @@ struct CeGradientEpi {
     w = on ? p.cw[row] : 0.f;
     lse2 = on ? p.lse2[row] : 1e30f;  // beyond the last row: p = 0, G = 0
   }
-  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0, uint32_t (&out)[1][16]) {
+  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0) {
+    if (row0 + pair_row >= blocks128) return;  // a block of rows that does not exist: nothing to store
     float g[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) g[i] = w * ex2f(fmaf(__uint_as_float(acc[i]), p.scale2, -lse2));
@@ -297,8 +288,7 @@ struct CeGradientEpi {
       for (int i = 0; i < 32; ++i)
         if (i >= nvalid) g[i] = 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) out[0][i] = pack_bf16x2(g[2 * i], g[2 * i + 1]);
+    store_row32<false>(p.gbuf + static_cast<size_t>(row0 + pair_row) * p.ldg + (col0 - p.g_col0), g, 32, true);
   }
   __device__ __forceinline__ void end(const PairTile&) {}
 };
@@ -331,7 +321,7 @@ __global__ void __launch_bounds__(256) ce_merge_kernel(const CeMergeParams p) {
   grid_dependency_wait();
   grid_launch_dependents();
   const int c = t < p.T ? p.cidx[t] : -1;
-  const int slots = 2 * p.plan[2];
+  const int slots = 4 * p.plan[2];
   float m = -INFINITY, s = 0.f;
   if (c >= 0) {
     for (int i = warp; i < slots; i += 8) {

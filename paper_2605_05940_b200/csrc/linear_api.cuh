@@ -99,14 +99,11 @@ cudaError_t launch_rows(const LinearParams& p, cudaStream_t st) {
 
 template <bool kY32, bool kKeepZ>
 int launch_linear_tiles(const npd_linear_args* a, const LinearParams& p, int sms, cudaStream_t st) {
-  CUtensorMap mx, mw, my, mz;
-  if (!make_map(&mx, a->x, a->K, a->M, a->ldx, 64, 128) || !make_map(&mw, a->weight, a->K, a->N, a->ldw, 64, 128) ||
-      !make_map(&my, a->y, a->N, a->M, a->ldy, kY32 ? 16 : 32, 128, kY32, true, true))
+  CUtensorMap mx, mw;
+  if (!make_map(&mx, a->x, a->K, a->M, a->ldx, 64, 128) || !make_map(&mw, a->weight, a->K, a->N, a->ldw, 64, 128))
     return NPD_ECUDA;
-  if (!kKeepZ) mz = my;
-  else if (!make_map(&mz, a->preact, a->N, a->M, a->ldz, 32, 128, false, true, true)) return NPD_ECUDA;
   const int pairs = std::max(1, std::min(p.mtiles * p.ntiles, sms / 2));
-  return launch_pair_tile<LinearEpi<kY32, kKeepZ>>(mx, mw, my, mz, p, pairs, st, false);
+  return launch_pair_tile<LinearEpi<kY32, kKeepZ>>(mx, mw, p, pairs, st, false);
 }
 
 }  // namespace
@@ -140,6 +137,10 @@ int npd_linear_fwd(const npd_linear_args* a, void* cuda_stream) {
   p.ldy = a->ldy;
   p.ldz = a->ldz;
   p.y_f32 = a->y_dtype == NPD_DTYPE_F32;
+  // whole 32-byte sectors per store where the rows allow it
+  const int ye = p.y_f32 ? 4 : 2;
+  p.wide_y = reinterpret_cast<uintptr_t>(a->y) % 32 == 0 && a->ldy * ye % 32 == 0;
+  p.wide_z = reinterpret_cast<uintptr_t>(a->preact) % 32 == 0 && a->ldz * 2 % 32 == 0;
   p.status = a->status;
   if (a->M <= rows_cfg::kRowsMax) {
     const cudaError_t e = a->M <= 8    ? launch_rows<1>(p, st)

@@ -26,10 +26,26 @@ constexpr float kLog2e = 1.442695040888963407360f;
 // 1 / (1 + e^-v); exact limits at both ends (e^-v overflows to infinity, whose reciprocal is 0).
 __device__ __forceinline__ float sigmoidf(float v) { return __fdividef(1.f, 1.f + ex2f(-kLog2e * v)); }
 
+// Normal distribution function, Phi(z) = erfc(-z / sqrt 2) / 2, by formula 7.1.26 of Abramowitz and Stegun's
+// Handbook of Mathematical Functions: erfc(x) = t (a1 + t (a2 + ...)) e^(-x^2), t = 1 / (1 + p x) for x >= 0, off by at
+// most 1.5e-7 (one unit of fp32 near 1).  Two special-function instructions and ten others; the library's
+// erfcf made the epilogue of a K = 1536 tile take three times as long as its MMAs (242 us against 141 us
+// with the tanh form at M = 8192, N = 6144).
+__device__ __forceinline__ float normal_cdf(float z) {
+  const float x = 0.707106781186547524401f * fabsf(z);
+  const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+  float s = fmaf(1.061405429f, t, -1.453152027f);
+  s = fmaf(s, t, 1.421413741f);
+  s = fmaf(s, t, -0.284496736f);
+  s = fmaf(s, t, 0.254829592f);
+  const float q = 0.5f * s * t * ex2f(-kLog2e * x * x);  // Phi(-|z|)
+  return z < 0.f ? q : 1.f - q;
+}
+
 __device__ __forceinline__ float act_value(int act, float z) {
   switch (act) {
     case kActRelu: return z < 0.f ? 0.f : z;  // NaN stays NaN
-    case kActGelu: return 0.5f * z * erfcf(-0.707106781186547524401f * z);
+    case kActGelu: return z * normal_cdf(z);
     case kActGeluTanh: return z * sigmoidf(2.f * kGeluK * z * fmaf(kGeluC, z * z, 1.f));  // (1 + tanh u) / 2 = 1 / (1 + e^-2u)
     case kActSilu: return z * sigmoidf(z);
     default: return z;
@@ -39,8 +55,7 @@ __device__ __forceinline__ float act_slope(int act, float z) {
   switch (act) {
     case kActRelu: return z > 0.f ? 1.f : 0.f;
     case kActGelu:
-      return 0.5f * erfcf(-0.707106781186547524401f * z) +
-             z * 0.398942280401432677940f * ex2f(-0.5f * kLog2e * z * z);  // Phi(z) + z phi(z)
+      return normal_cdf(z) + z * 0.398942280401432677940f * ex2f(-0.5f * kLog2e * z * z);  // Phi(z) + z phi(z)
     case kActGeluTanh: {
       // q (1 - q) is 0 long before |z| = 100; what multiplies it stays finite, since 0 * inf is not 0
       const float zc = fminf(fmaxf(z, -100.f), 100.f), z2 = zc * zc;
@@ -69,6 +84,7 @@ struct LinearParams {
   __nv_bfloat16* z;             // or NULL
   long long ldy, ldz;
   int y_f32;                    // linear_rows_kernel only: y and residual are fp32
+  int wide_y, wide_z;           // every row starts on a 32-byte boundary
   int mtiles, ntiles, group;    // tiles of 256 x 256; rows of tiles per group (see LinearWalk)
   int* status;
 };
@@ -101,24 +117,12 @@ template <bool kY32, bool kKeepZ>
 struct LinearEpi {
   using Params = LinearParams;
   using Walk = LinearWalk;
-  static constexpr int kOuts = kKeepZ ? 2 : 1;
-  static constexpr bool kF32 = kY32;
-  static __device__ __forceinline__ int steps(const Params& p, const PairTile& t, int half, int row0) {
-    const int cols = p.N - (t.tile * pair_cfg::BN + half * pair_cfg::BNH);
-    return row0 >= p.M || cols <= 0 ? 0 : min(4, (cols + 31) / 32);
-  }
-  static __device__ __forceinline__ bool keeps(const Params& p, const PairTile& t, int col) {
-    // A TMA store clips the matrix's last column to a 16-byte boundary, not to the element: where N lies beyond
-    // such a boundary, chunk() writes the 32 columns across the edge itself.
-    const int c = t.tile * pair_cfg::BN + col;
-    return p.N % 8 == 0 ? c < p.N : c / 32 * 32 + 32 <= p.N;
-  }
-  static __device__ __forceinline__ int out_col(const Params&, const PairTile& t) { return t.tile * pair_cfg::BN; }
   const Params& p;
-  int pair_row, half, lane, row;
+  int pair_row, quarter, lane, row;
   uint4 next[kY32 ? 8 : 4];  // residual of the next chunk: its loads run under the chunk before
-  __device__ __forceinline__ LinearEpi(const Params& p_, int pair_row_, int half_)
-      : p(p_), pair_row(pair_row_), half(half_), lane(threadIdx.x & 31), row(0) {}
+  float bias[2];             // of this lane's column in either chunk
+  __device__ __forceinline__ LinearEpi(const Params& p_, int pair_row_, int quarter_)
+      : p(p_), pair_row(pair_row_), quarter(quarter_), lane(threadIdx.x & 31), row(0), bias{0.f, 0.f} {}
   __device__ __forceinline__ void fetch(int col0) {
     constexpr int kE = kY32 ? 4 : 2, kPerVec = 16 / kE, kVecs = 32 / kPerVec;
     if (p.residual == nullptr || row >= p.M) return;
@@ -142,24 +146,26 @@ struct LinearEpi {
   }
   __device__ __forceinline__ void begin(const PairTile& t) {
     row = t.row0 + pair_row;
-    const int col0 = t.tile * pair_cfg::BN + half * pair_cfg::BNH;
+    const int col0 = t.tile * pair_cfg::BN + quarter * pair_cfg::BNQ;
     if (col0 < p.N) fetch(col0);
+    if (p.bias != nullptr) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bias[i] = col0 + 32 * i + lane < p.N ? linear_bias(p, col0 + 32 * i + lane) : 0.f;
+    }
   }
-  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0, uint32_t (&out)[(kY32 ? 2 : 1) + (kKeepZ ? 1 : 0)][16]) {
-    constexpr int kSub = kY32 ? 2 : 1;
+  __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0) {
+    const int n = p.N - col0;
+    if (n <= 0) return;  // the same for the whole warp
     float v[32];
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
     if (p.bias != nullptr) {
-      // one coalesced load per warp, handed round by shuffles
-      const float b = col0 + lane < p.N ? linear_bias(p, col0 + lane) : 0.f;
+      // loaded once per warp, a column per lane, and handed round by shuffles
+      const float b = col0 % pair_cfg::BNQ == 0 ? bias[0] : bias[1];
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] += __shfl_sync(0xffffffffu, b, i);
     }
-    if (kKeepZ) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) out[kSub][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    }
+    if (kKeepZ && row < p.M) store_row32<false>(p.z + static_cast<size_t>(row) * p.ldz + col0, v, n, p.wide_z != 0);
     switch (p.act) {  // the same for the whole grid
       case kActRelu: apply<kActRelu>(v); break;
       case kActGelu: apply<kActGelu>(v); break;
@@ -181,29 +187,11 @@ struct LinearEpi {
           }
         }
       }
-      const int last = (col0 / pair_cfg::BNH + 1) * pair_cfg::BNH;  // end of this half
+      const int last = (col0 / pair_cfg::BNQ + 1) * pair_cfg::BNQ;  // end of this quarter
       if (col0 + 32 < min(last, p.N)) fetch(col0 + 32);
     }
-    if (kY32) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) out[(i >> 4) % kSub][i & 15] = __float_as_uint(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) out[0][i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-    }
-    if (p.N % 8 != 0 && col0 + 32 > p.N && row < p.M) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        if (col0 + i >= p.N) continue;
-        const size_t at = static_cast<size_t>(row) * p.ldy + col0 + i;
-        if (kY32) static_cast<float*>(p.y)[at] = v[i];
-        else static_cast<__nv_bfloat16*>(p.y)[at] = __float2bfloat16_rn(v[i]);
-        if (kKeepZ) {
-          const uint32_t w = out[kSub][i / 2];
-          reinterpret_cast<uint16_t*>(p.z)[static_cast<size_t>(row) * p.ldz + col0 + i] = static_cast<uint16_t>(i & 1 ? w >> 16 : w);
-        }
-      }
-    }
+    if (row < p.M)
+      store_row32<kY32>(static_cast<char*>(p.y) + (static_cast<size_t>(row) * p.ldy + col0) * (kY32 ? 4 : 2), v, n, p.wide_y != 0);
   }
   template <int kAct>
   static __device__ __forceinline__ void apply(float (&v)[32]) {

@@ -305,8 +305,11 @@ int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const
   gp.nblocks = nblocks;
   gp.status = status;
   const int pairs = static_cast<int>(std::max<long long>(1, std::min<long long>(units, std::max(sms / 2, 1))));
-  if (set_smem(gemm_bf16_kernel, SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
-  const cudaError_t e = launch_ex(gemm_bf16_kernel, 2 * pairs, THREADS, SMEM_BYTES, st, pdl, maps[0], maps[1],
+  int form = 0;
+  for (int i = 0; i < nprob; ++i) form = std::max(form, gp.pr[i].ragged ? 2 : (gp.pr[i].alpha != 1.f ? 1 : 0));
+  auto k = form == 0 ? gemm_bf16_kernel<0> : (form == 1 ? gemm_bf16_kernel<1> : gemm_bf16_kernel<2>);
+  if (set_smem(k, SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
+  const cudaError_t e = launch_ex(k, 2 * pairs, THREADS, SMEM_BYTES, st, pdl, maps[0], maps[1],
                                   maps[2], maps[3], maps[4], maps[5], gp);
   ++g_launches;
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;

@@ -6,32 +6,28 @@
 // K-major bf16, 128-byte swizzle), and its tensor memory receives its own 128 rows of the tile for all 256
 // columns.  Two accumulators (all 512 columns of tensor memory) let the epilogue of a tile run under the
 // MMAs of the next one.  A stage of the operand ring is two k-steps of 64 deep (64 KB, eight MMAs per
-// hand-off): a hand-off costs the tensor pipe about 120 clocks whatever the stage holds.  Three stages, and
-// 32 KB for the output staging, fill the 227 KB of shared memory.
+// hand-off): a hand-off costs the tensor pipe about 120 clocks whatever the stage holds.  Three stages are what
+// the 227 KB of shared memory hold.
 //
-// CTA = 384 threads, one CTA per SM, persistent over the tiles its pair's walk yields:
+// CTA = 576 threads, one CTA per SM, persistent over the tiles its pair's walk yields:
 //   warp 0      TMA producer of this CTA's operand stages; the completion of both CTAs' loads is
 //               counted on the leader's "full" barrier
 //   warp 1      leader CTA (cluster rank 0) only: the MMA issuer of the pair.  In both CTAs this warp
 //               owns the tensor memory
-//   warps 2, 3  one storing thread each, for the left and the right half of a tile's columns
-//   warps 4-11  epilogue: warp w reads tensor-memory lanes 32*(w%4).., columns 128*((w-4)/4).., so that
-//               every thread owns one row and half of the tile's columns
-// An epilogue with results the size of the tile writes them, 128 rows x 64 bytes at a time, to a ring of
-// two staging buffers per half (64-byte swizzle); the storing thread hands them to TMA stores, which
-// clip them at the matrix's edges.  Roles meet at mbarriers only, and every wait is bounded.
+//   warps 2-17  epilogue: warp w reads tensor-memory lanes 32*(w%4).., columns 64*((w-2)/4).., so that
+//               every thread owns one row and a quarter of the tile's columns.  Sixteen warps, four per
+//               scheduler: with eight (half a tile each) an epilogue with an activation was bound by its
+//               own latencies and took longer than the MMAs of a K = 1536 tile
+// An epilogue stores results the size of the tile from registers, 64 bytes of a row per thread and chunk
+// (two full 32-byte sectors).  Staging them in shared memory for TMA stores was slower: the MMAs already
+// take most of the shared memory's bandwidth, so staging traffic slows the main loop down.  Roles meet at
+// mbarriers only, and every wait on one is bounded.
 //
-// Epi provides (all evaluated by every role alike unless said otherwise):
+// Epi provides (Walk is evaluated by every role alike):
 //   Params                     launch parameters, with `int* status` and `int ksteps`
-//   Walk(p, pair, pairs, rank) the tiles of a pair: bool next(PairTile&)
-//   kOuts                      tile-sized results per tile (0, 1 or 2); kF32 = the first is fp32, else bf16
-//                              (a second one is always bf16)
-//   steps(p, tile, half, row0) 32-column chunks of this half that have to be stored (0 .. 4)
-//   keeps(p, tile, col)        whether a staging buffer whose first column is `col` of the tile is stored
-//   out_col(p, tile)           column of the results that the tile's column 0 goes to
-//   Epi(p, row_local, half)    per epilogue thread; then for every tile begin(tile), for every chunk
-//                              chunk(acc[32], col0, out), and end(tile); out[i] is the i-th staging buffer's
-//                              64 bytes of this row: the first result's one (bf16) or two (fp32), then the second's
+//   Walk(p, pair, pairs)       the tiles of a pair: bool next(PairTile&)
+//   Epi(p, row_local, quarter) per epilogue thread; then for every tile begin(tile), for every chunk of 32
+//                              columns chunk(acc[32], col0), and end(tile)
 #pragma once
 
 #include "ptx_sm100.cuh"
@@ -45,33 +41,57 @@ struct PairTile {
   bool first, last; // of that sequence
 };
 
+// 32 consecutive results of a row.  `n` of them exist; `wide` = the address is on a 32-byte boundary (it is on
+// a 16-byte one in any case).
+template <bool kF32>
+__device__ __forceinline__ void store_row32(void* dst, const float (&v)[32], int n, bool wide) {
+  constexpr int kWords = kF32 ? 32 : 16;
+  uint32_t w[kWords];
+#pragma unroll
+  for (int i = 0; i < kWords; ++i)
+    w[i] = kF32 ? __float_as_uint(v[i % 32]) : pack_bf16x2(v[(2 * i) % 32], v[(2 * i + 1) % 32]);
+  uint32_t* p = static_cast<uint32_t*>(dst);
+  if (n >= 32 && wide) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]),
+                   "r"(w[i + 3]), "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7])
+                   : "memory");
+  } else if (n >= 32) {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) *reinterpret_cast<uint4*>(p + i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (i >= n) continue;
+      if (kF32) p[i] = w[i % kWords];
+      else reinterpret_cast<uint16_t*>(p)[i] = static_cast<uint16_t>(i & 1 ? w[i / 2] >> 16 : w[i / 2]);
+    }
+  }
+}
+
 namespace pair_cfg {
 constexpr int BM = 128, BN = 256, BK = 64, UK = 16;
 constexpr int BNH = BN / 2;
 constexpr int KS = 2, STAGES = 3;
 constexpr int A_BYTES = BM * BK * 2;
 constexpr int B_BYTES = BNH * BK * 2;
-constexpr int OUT_BYTES = 128 * 64;  // one staging buffer
-constexpr int OUT_BUFS = 2;          // per half
-constexpr int THREADS = 384;
+constexpr int EPI_WARPS = 16;
+constexpr int BNQ = BN / 4;          // columns of an epilogue warp
+constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int TMEM_COLS = 512;
 constexpr int OFF_A = 0;
 constexpr int OFF_B = OFF_A + STAGES * KS * A_BYTES;
-constexpr int OFF_OUT = OFF_B + STAGES * KS * B_BYTES;
-constexpr int OFF_BAR = OFF_OUT + 2 * OUT_BUFS * OUT_BYTES;
-constexpr int NUM_BARS = 2 * STAGES + 4 + 4 * OUT_BUFS;
+constexpr int OFF_BAR = OFF_B + STAGES * KS * B_BYTES;
+constexpr int NUM_BARS = 2 * STAGES + 4;
 constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
 }  // namespace pair_cfg
 
 template <class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_cfg::THREADS, 1)
 pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
-                 const __grid_constant__ CUtensorMap tmap_o0, const __grid_constant__ CUtensorMap tmap_o1,
                  const typename Epi::Params p) {
   using namespace pair_cfg;
-  constexpr int kOuts = Epi::kOuts;
-  constexpr int kSub = Epi::kF32 ? 2 : 1;                                     // staging buffers per chunk: first result,
-  constexpr int kPer = kOuts == 0 ? 1 : kSub + (kOuts > 1 ? 1 : 0);          // all results
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -86,8 +106,6 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
   const uint32_t empty0 = full0 + 8 * STAGES;
   const uint32_t tfull0 = empty0 + 8 * STAGES;
   const uint32_t tempty0 = tfull0 + 16;
-  const uint32_t ofull0 = tempty0 + 16;               // [half][OUT_BUFS]
-  const uint32_t oempty0 = ofull0 + 8 * 2 * OUT_BUFS;  // [half][OUT_BUFS]
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) {
@@ -96,18 +114,12 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull0 + 8 * b, 1);
-      mbar_init(tempty0 + 8 * b, 16);  // 8 epilogue warps of each CTA, counted in the leader
-    }
-    for (int i = 0; i < 2 * OUT_BUFS; ++i) {
-      mbar_init(ofull0 + 8 * i, 4);   // the four warps of the half
-      mbar_init(oempty0 + 8 * i, 1);  // the half's storing thread
+      mbar_init(tempty0 + 8 * b, 2 * EPI_WARPS);  // the epilogue warps of both CTAs, counted in the leader
     }
     *abort_flag = 0;
     fence_mbar_init();
     prefetch_tmap(&tmap_a);
     prefetch_tmap(&tmap_b);
-    if (kOuts > 0) prefetch_tmap(&tmap_o0);
-    if (kOuts > 1) prefetch_tmap(&tmap_o1);
   }
   if (warp == 1) tmem_alloc_pair(smem_u32(tmem_slot), TMEM_COLS);
   tc_fence_before_sync();
@@ -197,88 +209,34 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         if (ok) umma_commit_pair(tfull0 + 8 * buf);
       }
     }
-  } else if (warp < 4) {
-    // ---------------------- storing threads ----------------------
-    if (kOuts > 0 && lane == 0) {
-      const int half = warp - 2;
-      uint32_t oit = 0;
-      int prev = -1;  // buffer of the copy in flight
-      bool ok = true;
-      while (ok && walk.next(t)) {
-        const int row0 = t.row0 + static_cast<int>(rank) * BM;
-        const int n = Epi::steps(p, t, half, row0);
-        for (int j = 0; j < n * kPer && ok; ++j, ++oit) {
-          const int b = half * OUT_BUFS + static_cast<int>(oit % OUT_BUFS);
-          if (!(ok = mbar_wait(ofull0 + 8 * b, (oit / OUT_BUFS) & 1, abort_flag))) break;
-          const int c = j / kPer, which = j % kPer < kSub ? 0 : 1, sub = which == 0 ? j % kPer : 0;
-          const int col = half * BNH + c * 32 + sub * 16;  // within the tile
-          if (Epi::keeps(p, t, col))
-            tma_store_2d(which == 0 ? &tmap_o0 : &tmap_o1, smem_u32(smem + OFF_OUT + b * OUT_BYTES),
-                         Epi::out_col(p, t) + col, row0);
-          tma_store_commit();
-          if (prev >= 0) {
-            tma_store_wait_read<1>();  // the copy before this one has read its buffer
-            mbar_arrive(oempty0 + 8 * prev);
-          }
-          prev = b;
-        }
-      }
-      tma_store_wait_read<0>();
-      if (prev >= 0) mbar_arrive(oempty0 + 8 * prev);
-      tma_store_wait_all<0>();
-    }
   } else {
     // ---------------------- epilogue ----------------------
-    const int e = warp - 4;
-    const int lg = e & 3;     // == warp % 4: the lane group of tensor memory this warp may read
-    const int half = e >> 2;  // which 128 columns of the tile
-    const int row_local = lg * 32 + lane;
-    const uint32_t swz = static_cast<uint32_t>((row_local >> 1) & 3);  // 64-byte swizzle
-    Epi epi(p, static_cast<int>(rank) * BM + row_local, half);
-    uint32_t tile = 0, oit = 0;
+    const int e = warp - 2;
+    const int lg = warp & 3;     // the lane group of tensor memory this warp may read
+    const int quarter = e >> 2;  // which 64 columns of the tile
+    Epi epi(p, static_cast<int>(rank) * BM + lg * 32 + lane, quarter);
+    uint32_t tile = 0;
     bool ok = true;
     for (; ok && walk.next(t); ++tile) {
       const uint32_t buf = tile & 1, tph = (tile >> 1) & 1;
-      const int row0 = t.row0 + static_cast<int>(rank) * BM;
       epi.begin(t);
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, tph, abort_flag)))) break;
       tc_fence_after_sync();
-      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(lg * 32) << 16) + buf * BN + half * BNH;
-      const int n = kOuts > 0 ? Epi::steps(p, t, half, row0) : BNH / 32;
-      // once everything this warp needs of an accumulator is in registers it may be overwritten
-      auto release = [&]() {
-        tc_fence_before_sync();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
-      };
-      if (n == 0) release();
+      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(lg * 32) << 16) + buf * BN + quarter * BNQ;
 #pragma unroll 1
-      for (int c = 0; c < n && ok; ++c) {
+      for (int c = 0; c < BNQ / 32; ++c) {
         uint32_t acc[32];
         __syncwarp();  // the epilogue's branches may have parted the warp
         tmem_ld32(taddr + c * 32, acc);
         tmem_ld_wait();
-        if (c == n - 1) release();
-        uint32_t out[kPer][16];
-        epi.chunk(acc, t.tile * BN + half * BNH + c * 32, out);
-        if (kOuts > 0) {
-#pragma unroll
-          for (int s = 0; s < kPer; ++s, ++oit) {
-            const int b = half * OUT_BUFS + static_cast<int>(oit % OUT_BUFS);
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(oempty0 + 8 * b, ((oit / OUT_BUFS) & 1) ^ 1, abort_flag)))) break;
-            uint8_t* orow = smem + OFF_OUT + b * OUT_BYTES + row_local * 64;
-            const uint32_t* w = out[s];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-              *reinterpret_cast<uint4*>(orow + ((static_cast<uint32_t>(q) ^ swz) << 4)) =
-                  make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ofull0 + 8 * b);
-          }
+        if (c == BNQ / 32 - 1) {
+          // everything this warp needs of the accumulator is in registers: it may be overwritten
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
         }
+        epi.chunk(acc, t.tile * BN + quarter * BNQ + c * 32);
       }
-      if (!ok) break;
       epi.end(t);
     }
   }
