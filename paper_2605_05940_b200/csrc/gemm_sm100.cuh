@@ -68,6 +68,8 @@ struct GemmProblem {
 struct GemmParams {
   GemmProblem pr[2];
   int nprob;           // 1 or 2
+  int balance;         // 1: two problems of whole tiles with extents known on the host, dealt so that the
+                       // pairs' k-steps come out (almost) equal; see GemmWalk
   const int* nblocks;  // device; read only when a problem has dyn_m / dyn_k
   int* status;         // device status word
 };
@@ -125,8 +127,13 @@ struct GemmWalk {
   int mt0, m_lone;     // row tiles of problem 0; the first m_lone of them go to the lone pairs
   int mine0;           // units of problem 0 this pair takes
   int lone_first;      // lone pair: its first tile (n fastest) of problem 0
+  // balanced mode: the problem with the longer k goes first, its tiles round robin (pairs 0..extra-1 take one
+  // more); then the tiles of the other one, `few` to each of those pairs and `many` to each of the others
+  int balanced, big, extra, few, many;
 
   // nb = number of 128-row blocks behind the device-side extents (dyn_m / dyn_k)
+  // kBalance: p.balance is looked at (left out of the kernels that never set it)
+  template <bool kBalance = true>
   __host__ __device__ __forceinline__ void init(const GemmParams& p, int nb, int c_, int C_) {
     using namespace gemm_cfg;
     c = c_;
@@ -134,6 +141,7 @@ struct GemmWalk {
     i = 0;
     pos = end = 0;
     grouped = 0;
+    balanced = 0;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       pr[q] = p.pr[q];
@@ -141,6 +149,26 @@ struct GemmWalk {
       if (pr[q].dyn_k) pr[q].K = 128 * nb;
       tiles[q] = q < p.nprob ? ((pr[q].M + PM - 1) / PM) * ((pr[q].N + BN - 1) / BN) : 0;
       ksteps[q] = (pr[q].K + BK - 1) / BK;
+    }
+    if (kBalance && p.balance && p.nprob == 2 && ksteps[0] > 0 && ksteps[1] > 0) {
+      balanced = 1;
+      big = ksteps[1] > ksteps[0] ? 1 : 0;
+      const long long kb = ksteps[big], ks = ksteps[1 - big], nb_ = tiles[big], ns = tiles[1 - big];
+      const long long q = nb_ / C;
+      extra = static_cast<int>(nb_ % C);
+      // smallest level of k-steps (to an eighth of a short tile) up to which the short tiles all fit
+      long long level = (nb_ * kb + ns * ks + C - 1) / C, a, b;
+      for (;;) {
+        a = level - (q + 1) * kb;
+        a = a > 0 ? a / ks : 0;
+        b = level - q * kb;
+        b = b > 0 ? b / ks : 0;
+        if (a * extra + b * (C - extra) >= ns) break;
+        level += (ks + 7) / 8;
+      }
+      few = static_cast<int>(a);
+      many = static_cast<int>(b);
+      return;
     }
     tn = (pr[0].N + BN - 1) / BN;
     G = tn > 0 ? C / tn : 0;
@@ -197,7 +225,25 @@ struct GemmWalk {
     }
   }
 
+  template <bool kBalance = true>
   __host__ __device__ __forceinline__ bool next(int& prob, GemmUnit& u) {
+    if (kBalance && balanced) {
+      const int mine = tiles[big] / C + (c < extra ? 1 : 0);
+      if (i < mine) {
+        prob = big;
+        u = gemm_tile_unit(pr[big], c + i * C, 0, ksteps[big]);
+        ++i;
+        return true;
+      }
+      const int j = i - mine;  // j-th round of the short tiles; after `few` of them only pairs extra.. go on
+      if (j >= (c < extra ? few : many)) return false;
+      const int v = j < few ? j * C + c : few * C + (j - few) * (C - extra) + (c - extra);
+      if (v >= tiles[1 - big]) return false;
+      prob = 1 - big;
+      u = gemm_tile_unit(pr[1 - big], v, 0, ksteps[1 - big]);
+      ++i;
+      return true;
+    }
     if (grouped) {
       if (i < mine0) {
         prob = 0;
@@ -265,8 +311,8 @@ __device__ __forceinline__ void gemm_store_edge(void* out, size_t at, int n, boo
   }
 }
 
-// kForm: 0 = plain, 1 = the problems have factors other than 1, 2 = factors and ragged last columns.  The
-// distillation step's contractions are plain, and run 0.8 % faster without the code for the rest.
+// kForm: 0 = plain, 1 = the problems have factors other than 1, 2 = factors, ragged last columns and the balanced
+// deal.  The distillation step's contractions are plain, and run 0.8 % faster without the code for the rest.
 template <int kForm>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(gemm_cfg::THREADS, 1)
 gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_constant__ CUtensorMap tmap_b0,
@@ -274,6 +320,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
                  const __grid_constant__ CUtensorMap tmap_b1, const __grid_constant__ CUtensorMap tmap_o1,
                  const GemmParams p) {
   using namespace gemm_cfg;
+  constexpr bool kBal = kForm == 2;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -331,7 +378,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
   grid_launch_dependents();
   GemmWalk walk;
   const bool dyn = p.pr[0].dyn_m || p.pr[0].dyn_k || p.pr[1].dyn_m || p.pr[1].dyn_k;
-  walk.init(p, dyn ? __ldg(p.nblocks) : 0, cluster_id, num_clusters);
+  walk.template init<kBal>(p, dyn ? __ldg(p.nblocks) : 0, cluster_id, num_clusters);
 
   if (warp == 0) {
     // ------------------------------ TMA producer ------------------------------
@@ -340,7 +387,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
       bool ok = true;
       int prob;
       GemmUnit u;
-      while (ok && walk.next(prob, u)) {
+      while (ok && walk.template next<kBal>(prob, u)) {
         const GemmProblem& g = prob ? walk.pr[1] : walk.pr[0];
         const CUtensorMap* ta = prob ? &tmap_a1 : &tmap_a0;
         const CUtensorMap* tb = prob ? &tmap_b1 : &tmap_b0;
@@ -402,7 +449,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
       bool ok = true;
       int prob;
       GemmUnit u;
-      for (; ok && walk.next(prob, u); ++tile) {
+      for (; ok && walk.template next<kBal>(prob, u); ++tile) {
         const GemmProblem& g = prob ? walk.pr[1] : walk.pr[0];
         const uint32_t idesc = umma_idesc_bf16(PM, BNS, g.a_mn != 0, g.b_mn != 0);
         // the accumulators are free once every epilogue warp of the pair has read the last tile
@@ -452,7 +499,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
     if (storer) {
       if (lane == 0) {
         int prev = -1;  // buffer of the copy in flight
-        while (ok && walk.next(prob, u)) {
+        while (ok && walk.template next<kBal>(prob, u)) {
           const GemmProblem& g = prob ? walk.pr[1] : walk.pr[0];
           const CUtensorMap* to = prob ? &tmap_o1 : &tmap_o0;
           int c0, step;
@@ -486,7 +533,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
       const int row_local = lg * 32 + lane;
       const uint32_t swz = static_cast<uint32_t>((row_local >> 1) & 3);  // 64-byte swizzle
       uint32_t tile = 0;
-      for (; ok && walk.next(prob, u); ++tile) {
+      for (; ok && walk.template next<kBal>(prob, u); ++tile) {
         const GemmProblem& g = prob ? walk.pr[1] : walk.pr[0];
         const bool no_k = u.kt0 == u.kt1;           // empty k range: the accumulators hold nothing, D = 0
         int c0, step;

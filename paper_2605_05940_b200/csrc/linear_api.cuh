@@ -246,7 +246,7 @@ int npd_linear_bwd(const npd_linear_args* a, void* cuda_stream) {
     pr[n] = gx;
     ops[n++] = ox;
   }
-  return launch_gemm(n, pr, ops, nullptr, 0, status, di.sms, st, true);
+  return launch_gemm(n, pr, ops, nullptr, 0, status, di.sms, st, true, true);
 }
 
 }  // extern "C"

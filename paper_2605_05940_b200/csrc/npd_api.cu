@@ -274,7 +274,7 @@ void chunk_problems(int d, int cols, bool dw_f32, bool dw_accumulate, GemmProble
 // One launch for one or two problems (see gemm_sm100.cuh for how the units are dealt).
 // An extent only known on the device (dyn_m / dyn_k) is 128 * max_blocks as far as the maps go.
 int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const int* nblocks,
-                int max_blocks, int* status, int sms, cudaStream_t st, bool pdl = false) {
+                int max_blocks, int* status, int sms, cudaStream_t st, bool pdl = false, bool balance = false) {
   using namespace gemm_cfg;
   CUtensorMap maps[6];
   GemmParams gp{};
@@ -302,10 +302,11 @@ int launch_gemm(int nprob, const GemmProblem* pr, const GemmOperands* ops, const
       units += static_cast<long long>((am + PM - 1) / PM) * ((g.N + BN - 1) / BN) * g.k_splits;
   }
   gp.nprob = nprob;
+  gp.balance = balance ? 1 : 0;
   gp.nblocks = nblocks;
   gp.status = status;
   const int pairs = static_cast<int>(std::max<long long>(1, std::min<long long>(units, std::max(sms / 2, 1))));
-  int form = 0;
+  int form = balance ? 2 : 0;
   for (int i = 0; i < nprob; ++i) form = std::max(form, gp.pr[i].ragged ? 2 : (gp.pr[i].alpha != 1.f ? 1 : 0));
   auto k = form == 0 ? gemm_bf16_kernel<0> : (form == 1 ? gemm_bf16_kernel<1> : gemm_bf16_kernel<2>);
   if (set_smem(k, SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
