@@ -87,7 +87,7 @@ LinearPlan linear_plan(const npd_linear_args* a, int sms) {
   size_t off = 1024;  // status word first, as in the other workspaces
   if (a->activation != NPD_ACT_NONE) off = align_up(off + 2 * static_cast<size_t>(a->M) * pl.lddz, 1024);
   pl.off_part = off;
-  off = align_up(off + sizeof(float) * static_cast<size_t>(pl.row_blocks) * a->N, 1024);
+  off = align_up(off + sizeof(float) * static_cast<size_t>(pl.row_blocks) * pl.lddz, 1024);
   pl.total = off;
   return pl;
 }
@@ -196,6 +196,7 @@ int npd_linear_bwd(const npd_linear_args* a, void* cuda_stream) {
     gp.lddy = a->lddy;
     gp.ldz = a->ldz;
     gp.lddz = pl.lddz;
+    gp.ldpart = pl.lddz;  // a multiple of 8
     gp.part = a->dbias != nullptr ? reinterpret_cast<float*>(ws + pl.off_part) : nullptr;
     if (act) {
       dz = gp.dz;
@@ -210,8 +211,8 @@ int npd_linear_bwd(const npd_linear_args* a, void* cuda_stream) {
                                false, gp);
     ++g_launches;
     if (e == cudaSuccess && a->dbias != nullptr) {
-      e = launch_dim(column_sum_kernel, dim3(static_cast<unsigned>((a->N + 31) / 32), 1), 512, 0, st, true, gp.part, pl.row_blocks,
-                      a->N, 0, a->N, a->dbias, nullptr, nullptr);
+      e = launch_dim(column_sum_kernel, dim3(static_cast<unsigned>((a->N + 31) / 32)), 1024, 0, st, true, gp.part, pl.row_blocks,
+                     gp.ldpart, a->N, a->dbias);
       ++g_launches;
     }
     if (e != cudaSuccess) return NPD_ECUDA;

@@ -316,8 +316,8 @@ struct LinearGradParams {
   const __nv_bfloat16* dy;
   const __nv_bfloat16* z;
   __nv_bfloat16* dz;     // or NULL
-  long long lddy, ldz, lddz;
-  float* part;           // [gridDim.y][N] or NULL
+  long long lddy, ldz, lddz, ldpart;
+  float* part;           // [gridDim.y][ldpart] or NULL
 };
 
 template <int kAct>
@@ -350,11 +350,11 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const LinearGradParams p
   for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = s.v[i];
   __syncthreads();
   const int col = blockIdx.x * 256 + threadIdx.x;
-  if (col >= p.N) return;
+  if (col >= p.ldpart) return;  // columns beyond N hold zeros
   float t = 0.f;
 #pragma unroll
   for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
-  p.part[static_cast<size_t>(blockIdx.y) * p.N + col] = t;
+  p.part[static_cast<size_t>(blockIdx.y) * p.ldpart + col] = t;
 }
 
 }  // namespace npd

@@ -33,7 +33,7 @@ bool bad_overlap(const Extent& out, const Extent& in, bool in_place) {
 }
 
 struct NormPlan {
-  int vec, threads, smem, grid;
+  int vec, threads, smem, grid, part_d;
   size_t ws;
 };
 
@@ -43,13 +43,14 @@ NormPlan norm_plan(const npd_norm_args* a, int sms, bool backward) {
   pl.vec = a->d <= kMaxSmallD ? 1 : (a->d <= 2 * kMaxSmallD ? 2 : 4);
   const int per = 8 * pl.vec;
   pl.threads = ((a->d + per - 1) / per + 31) / 32 * 32;
-  pl.smem = backward && pl.vec > 1 ? 3 * a->d * static_cast<int>(sizeof(float)) : 0;
+  pl.smem = backward && pl.vec > 1 ? 2 * a->d * static_cast<int>(sizeof(float)) : 0;  // sums over rows
   // Resident CTAs per SM, by threads and (an estimate of) registers: every CTA goes through its share
   // of the rows.  Several per SM, so that one CTA's barriers run under another one's loads.
-  int per_sm = (backward || pl.vec > 1 ? 512 : 640) / pl.threads;
+  int per_sm = (pl.vec > 1 ? 512 : (!backward ? 1024 : (pl.threads <= 256 ? 816 : 512))) / pl.threads;
   per_sm = std::max(1, std::min(per_sm, 16));
   pl.grid = std::min(a->T, sms * per_sm);
-  pl.ws = align_up(sizeof(float) * 3 * static_cast<size_t>(a->d) * pl.grid, 1024);
+  pl.part_d = (a->d + 3) / 4 * 4;
+  pl.ws = align_up(sizeof(float) * 2 * static_cast<size_t>(pl.part_d) * pl.grid, 1024);
   return pl;
 }
 
@@ -174,6 +175,14 @@ NormParams norm_params(const npd_norm_args* a, bool backward) {
   return p;
 }
 
+template <bool kF32>
+void (*norm_bwd_pick(const NormPlan& pl, bool full))(NormParams) {
+  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, false, 512, 1>;
+  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, false, 512, 1>;
+  if (pl.threads <= 256) return full ? norm_bwd_kernel<kF32, 1, true, 256, 3> : norm_bwd_kernel<kF32, 1, false, 256, 3>;
+  return full ? norm_bwd_kernel<kF32, 1, true, 512, 1> : norm_bwd_kernel<kF32, 1, false, 512, 1>;
+}
+
 }  // namespace
 
 extern "C" {
@@ -215,6 +224,7 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   if (di.cc_major != 10) return NPD_EARCH;
   const NormPlan pl = norm_plan(a, di.sms, true);
   NormParams p = norm_params(a, true);
+  p.part_d = pl.part_d;
   if (p.want != 0) {
     if (a->workspace == nullptr || (reinterpret_cast<uintptr_t>(a->workspace) & 15u) || a->workspace_bytes < pl.ws)
       return NPD_EWORKSPACE;
@@ -222,17 +232,18 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   }
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  auto k = pl.vec == 1   ? (sf ? norm_bwd_kernel<true, 1> : norm_bwd_kernel<false, 1>)
-           : pl.vec == 2 ? (sf ? norm_bwd_kernel<true, 2> : norm_bwd_kernel<false, 2>)
-                         : (sf ? norm_bwd_kernel<true, 4> : norm_bwd_kernel<false, 4>);
-  if (pl.smem > 0 && set_smem(k, 3 * norm_cfg::kMaxD * static_cast<int>(sizeof(float))) != NPD_OK) return NPD_ECUDA;
-  cudaError_t e = launch_ex(k, pl.grid, pl.threads, pl.smem, st, false, p);
+  const bool full = pl.vec == 1 && a->d % 256 == 0 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr &&
+                    p.dres != nullptr && (p.gate == nullptr || p.ldg == 0);
+  auto k = sf ? norm_bwd_pick<true>(pl, full) : norm_bwd_pick<false>(pl, full);
+  const int smem = full && !sf ? norm_cfg::kRing * pl.threads * 16 * 4 : pl.smem;
+  if (smem > 0 && set_smem(k, norm_cfg::kMaxSmem) != NPD_OK) return NPD_ECUDA;
+  cudaError_t e = launch_ex(k, pl.grid, pl.threads, smem, st, false, p);
   ++g_launches;
   if (e != cudaSuccess) return NPD_ECUDA;
   if (p.want != 0) {
     float* shared_dgate = (p.want & 4) ? static_cast<float*>(a->d_gate) : nullptr;
-    e = launch_dim(column_sum_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 3), 512, 0, st, true, p.part, pl.grid,
-                   3ll * a->d, a->d, a->d, a->d_pre_weight, a->d_post_weight, shared_dgate);
+    e = launch_dim(norm_sums_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 2), 1024, 0, st, true, p, pl.grid,
+                   a->d_pre_weight, a->d_post_weight, shared_dgate);
     ++g_launches;
   }
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;

@@ -47,7 +47,8 @@ struct NormParams {
   void* dres;                 // stream type or NULL
   __nv_bfloat16* dgate;       // per-token gate gradient, or NULL
   long long lddy, lddh, lddx, lddres, lddgate;
-  float* part;                // [gridDim][3][d] partial sums over rows: w_pre, w_post, shared gate
+  float* part;                // [gridDim][2][part_d] partial sums over rows: of dy h r_h, and S (see norm_bwd_kernel)
+  int part_d;                 // d rounded up to a multiple of 4
   int want;                   // bit 0: w_pre, bit 1: w_post, bit 2: shared gate
 };
 
@@ -59,6 +60,8 @@ constexpr int kMaxD = 16384;
 // data of two vectors alone fill the registers, and a row is then long enough to cover its latency.
 constexpr int kMaxSmallD = 4096;
 constexpr int kMaxThreads = 512;
+constexpr int kMaxSmem = 2 * kMaxD * 4;  // dynamic shared memory a launch may ask for: sums over the widest row
+constexpr int kRing = 2;  // rows in flight per CTA of the backward
 }  // namespace norm_cfg
 
 // ---- eight consecutive elements ----
@@ -164,40 +167,137 @@ __device__ __forceinline__ V8 gain8(const void* w, int w_f32, float offset, int 
   return o;
 }
 
-// Sums of N values over the block, the same in every thread.  One barrier; the caller alternates
-// `buf` so that a second call may write while slow threads still read the first one's numbers.
+// ---- the same as four pairs for the packed fp32 instructions (two results per instruction and thread: with
+// scalar ones these kernels are bound by the instructions they issue, not by memory) ----
+struct P8 {
+  unsigned long long p[4];
+};
+__device__ __forceinline__ unsigned long long pair2(float lo, float hi) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ float2 unpair2(unsigned long long a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+  return r;
+}
+__device__ __forceinline__ unsigned long long fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ unsigned long long mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float sum2(unsigned long long a) {
+  const float2 v = unpair2(a);
+  return v.x + v.y;
+}
+__device__ __forceinline__ P8 pack8(const V8& a) {
+  P8 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o.p[i] = pair2(a.v[2 * i], a.v[2 * i + 1]);
+  return o;
+}
+template <bool kF32>
+__device__ __forceinline__ P8 pairs8(const Raw8<kF32>& r) {
+  return pack8(unpack8<kF32>(r));
+}
+template <bool kF32>
+__device__ __forceinline__ void store8(void* row, int c, int d, const P8& a) {
+  V8 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 q = unpair2(a.p[i]);
+    v.v[2 * i] = q.x;
+    v.v[2 * i + 1] = q.y;
+  }
+  store8<kF32>(row, c, d, v);
+}
+
+// ---- a ring of rows in shared memory, filled by asynchronous copies; slot s of a stage holds 16 bytes of every
+// thread, and every thread copies and reads only its own, so the ring needs no barrier ----
+__device__ __forceinline__ void async_copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Waits until at most kPending of this thread's newest groups are in flight.
+template <int kPending>
+__device__ __forceinline__ void async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory");
+}
+__device__ __forceinline__ uint4 ring_get(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
+// Sums of N values over the block, the same in every thread, in a fixed order.  One barrier; the caller
+// alternates `buf` so that a second call may write while slow threads still read the first one's numbers.
+// At most 16 warps; the places of warps that do not exist hold zeros.
 template <int N>
-__device__ __forceinline__ void block_sum(float (&s)[N], float (*buf)[N]) {
+struct SumBuf {
+  float4 v[N][4];
+};
+template <int N>
+__device__ __forceinline__ void clear_sums(SumBuf<N>* buf, int count) {
+  float* f = reinterpret_cast<float*>(buf);
+  for (int i = threadIdx.x; i < count * N * 16; i += blockDim.x) f[i] = 0.f;
+}
+template <int N>
+__device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int k = 0; k < N; ++k) s[k] = warp_sum(s[k]);
   if (warps == 1) return;
   if (lane == 0) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) buf[warp][k] = s[k];
+    for (int k = 0; k < N; ++k) reinterpret_cast<float*>(&buf.v[k][0])[warp] = s[k];
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < N; ++k) s[k] = warp_sum(lane < warps ? buf[lane][k] : 0.f);
+  for (int k = 0; k < N; ++k) {
+    const float4 a = buf.v[k][0], b = buf.v[k][1];
+    s[k] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w));
+    if (warps > 8) {
+      const float4 c = buf.v[k][2], e = buf.v[k][3];
+      s[k] += ((c.x + c.y) + (c.z + c.w)) + ((e.x + e.y) + (e.z + e.w));
+    }
+  }
 }
+
+// What is missing in a call costs no branches in the arithmetic: a missing gain or gate is a gain of 1, a
+// missing operand zeros, and a branch without a norm has r_x = 1.
 
 // Forward.  kVec vectors of eight per thread; vector j of a thread starts at 8 * (threadIdx + j * blockDim).
 template <bool kF32, int kVec>
-__global__ void __launch_bounds__(norm_cfg::kMaxThreads) norm_fwd_kernel(const NormParams p) {
-  __shared__ float red[4][32][1];
-  constexpr bool kHold = kVec == 1;  // gains held in registers
+__global__ void __launch_bounds__(norm_cfg::kMaxThreads, kVec == 1 ? 2 : 1) norm_fwd_kernel(const NormParams p) {
+  __shared__ SumBuf<1> red[4];
+  constexpr bool kHold = kVec == 1;  // gains held in registers, the next row's loads in flight
+  constexpr size_t es = kF32 ? 4 : 2;
   const int nt = blockDim.x;
   const float inv_d = 1.f / static_cast<float>(p.d);
-  V8 wp[kVec], wq[kVec], gs[kVec];
-  const bool shared_gate = p.gate != nullptr && p.ldg == 0;
+  const bool token_gate = p.gate != nullptr && p.ldg != 0;
+  P8 wp[kVec], wq[kVec];  // gain of the branch times a shared gate; gain of y
   grid_dependency_wait();
   grid_launch_dependents();
-  if (kHold) {
-    const int c = 8 * threadIdx.x;
-    wp[0] = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
-    wq[0] = gain8(p.w_pre, p.w_f32, p.offset, c, p.d);
-    if (shared_gate) gs[0] = unpack8<false>(load8<false>(p.gate, c, p.d));
-  }
+  auto gains = [&](int j) {
+    const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+    V8 w = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
+    if (p.gate != nullptr && !token_gate) {
+      const V8 g = unpack8<false>(load8<false>(p.gate, c, p.d));
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w.v[i] *= g.v[i];
+    }
+    wp[j] = pack8(w);
+    wq[j] = pack8(gain8(p.w_pre, p.w_f32, p.offset, c, p.d));
+  };
+  if (kHold) gains(0);
+  clear_sums(red, 4);
+  __syncthreads();
   struct Row {
     Raw8<false> x[kVec], g[kVec];
     Raw8<kF32> r[kVec];
@@ -209,123 +309,8 @@ __global__ void __launch_bounds__(norm_cfg::kMaxThreads) norm_fwd_kernel(const N
       const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
       o.x[j] = p.x != nullptr ? load8<false>(p.x + static_cast<size_t>(t) * p.ldx, c, p.d) : zero8<false>();
       o.r[j] = p.residual != nullptr
-                  ? load8<kF32>(static_cast<const char*>(p.residual) + static_cast<size_t>(t) * p.ldr * (kF32 ? 4 : 2), c, p.d)
+                  ? load8<kF32>(static_cast<const char*>(p.residual) + static_cast<size_t>(t) * p.ldr * es, c, p.d)
                   : zero8<kF32>();
-      if (p.gate != nullptr && !shared_gate) o.g[j] = load8<false>(p.gate + static_cast<size_t>(t) * p.ldg, c, p.d);
-    }
-    return o;
-  };
-  int t = blockIdx.x, par = 0;
-  Row next;
-  if (kHold && t < p.T) next = fetch(t);
-  for (; t < p.T; t += gridDim.x, par ^= 1) {
-    const Row cur = kHold ? next : fetch(t);
-    if (kHold && t + static_cast<int>(gridDim.x) < p.T) next = fetch(t + gridDim.x);
-    V8 r[kVec];
-    float scale = p.branch_scale;
-    if (p.post) {
-      float s[1] = {0.f};
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const V8 x = unpack8<false>(cur.x[j]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] = fmaf(x.v[i], x.v[i], s[0]);
-      }
-      block_sum<1>(s, red[2 * par]);
-      scale *= rsqrtf(fmaf(s[0], inv_d, p.eps));
-    }
-    float s[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (!kHold) {
-        if (p.post) wp[j] = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
-        if (shared_gate) gs[j] = unpack8<false>(load8<false>(p.gate, c, p.d));
-      }
-      const V8 x = unpack8<false>(cur.x[j]);
-      r[j] = unpack8<kF32>(cur.r[j]);
-      V8 g;
-      if (p.gate != nullptr) g = shared_gate ? gs[j] : unpack8<false>(cur.g[j]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float b = x.v[i] * scale;
-        if (p.post) b *= wp[j].v[i];
-        if (p.gate != nullptr) b *= g.v[i];
-        const float h = fmaf(p.res_scale, r[j].v[i], b);
-        r[j].v[i] = h;
-        s[0] = fmaf(h, h, s[0]);
-      }
-      if (p.h != nullptr)
-        store8<kF32>(static_cast<char*>(p.h) + static_cast<size_t>(t) * p.ldh * (kF32 ? 4 : 2), c, p.d, r[j]);
-    }
-    if (p.y == nullptr) continue;
-    block_sum<1>(s, red[2 * par + 1]);
-    const float rh = rsqrtf(fmaf(s[0], inv_d, p.eps));
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (!kHold) wq[j] = gain8(p.w_pre, p.w_f32, p.offset, c, p.d);
-      V8 o;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) o.v[i] = r[j].v[i] * rh * wq[j].v[i];
-      store8<false>(p.y + static_cast<size_t>(t) * p.ldy, c, p.d, o);
-    }
-  }
-}
-
-// Backward.  The sums over rows live in registers (kVec == 1) or in shared memory (dynamic, [3][d]).
-template <bool kF32, int kVec>
-__global__ void __launch_bounds__(norm_cfg::kMaxThreads) norm_bwd_kernel(const NormParams p) {
-  __shared__ float red3[2][32][3];
-  __shared__ float red1[2][32][1];
-  extern __shared__ float acc_smem[];
-  constexpr bool kHold = kVec == 1;
-  const int nt = blockDim.x;
-  const float inv_d = 1.f / static_cast<float>(p.d);
-  const bool shared_gate = p.gate != nullptr && p.ldg == 0, token_gate = p.gate != nullptr && p.ldg != 0;
-  V8 wp[kVec], wq[kVec], gs[kVec];
-  V8 acc[3];  // kHold: sums over this CTA's rows of dy h r_h, dn x r_x, b n dh
-  if (kHold) {
-    const int c = 8 * threadIdx.x;
-    grid_dependency_wait();
-    wp[0] = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
-    wq[0] = gain8(p.w_pre, p.w_f32, p.offset, c, p.d);
-    if (shared_gate) gs[0] = unpack8<false>(load8<false>(p.gate, c, p.d));
-#pragma unroll
-    for (int a = 0; a < 3; ++a)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) acc[a].v[i] = 0.f;
-  } else {
-    // every thread clears, adds to and reads back its own columns only: no barrier needed
-    for (int a = 0; a < 3; ++a)
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        for (int i = 0; i < 8; ++i) {
-          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
-          if (c < p.d) acc_smem[a * p.d + c] = 0.f;
-        }
-    grid_dependency_wait();
-  }
-  struct Row {
-    Raw8<false> dy[kVec], x[kVec], g[kVec];
-    Raw8<kF32> h[kVec], dh[kVec];
-  };
-  const size_t es = kF32 ? 4 : 2;
-  auto fetch = [&](int t) {
-    Row o;
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (p.dy != nullptr) {
-        o.dy[j] = load8<false>(p.dy + static_cast<size_t>(t) * p.lddy, c, p.d);
-        o.h[j] = load8<kF32>(static_cast<const char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, p.d);
-      } else {
-        o.dy[j] = zero8<false>();
-        o.h[j] = zero8<kF32>();
-      }
-      o.dh[j] = p.dh != nullptr ? load8<kF32>(static_cast<const char*>(p.dh) + static_cast<size_t>(t) * p.lddh * es, c, p.d)
-                                : zero8<kF32>();
-      o.x[j] = p.x != nullptr ? load8<false>(p.x + static_cast<size_t>(t) * p.ldx, c, p.d) : zero8<false>();
       if (token_gate) o.g[j] = load8<false>(p.gate + static_cast<size_t>(t) * p.ldg, c, p.d);
     }
     return o;
@@ -336,130 +321,336 @@ __global__ void __launch_bounds__(norm_cfg::kMaxThreads) norm_bwd_kernel(const N
   for (; t < p.T; t += gridDim.x, par ^= 1) {
     const Row cur = kHold ? next : fetch(t);
     if (kHold && t + static_cast<int>(gridDim.x) < p.T) next = fetch(t + gridDim.x);
-    V8 vv[kVec];
-    float s[3] = {0.f, 0.f, 0.f};  // sum h^2, sum g h, sum x^2
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (!kHold) wq[j] = gain8(p.w_pre, p.w_f32, p.offset, c, p.d);
-      const V8 dy = unpack8<false>(cur.dy[j]), h = unpack8<kF32>(cur.h[j]), x = unpack8<false>(cur.x[j]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s[0] = fmaf(h.v[i], h.v[i], s[0]);
-        s[1] = fmaf(dy.v[i] * wq[j].v[i], h.v[i], s[1]);
-        s[2] = fmaf(x.v[i], x.v[i], s[2]);
-      }
-    }
-    block_sum<3>(s, red3[par]);
-    const float rh = p.dy != nullptr ? rsqrtf(fmaf(s[0], inv_d, p.eps)) : 0.f;
-    const float ch = rh * rh * s[1] * inv_d;
-    const float rx = p.post ? rsqrtf(fmaf(s[2], inv_d, p.eps)) : 1.f;
-    float q[1] = {0.f};  // sum v x
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (!kHold) {
-        wq[j] = gain8(p.w_pre, p.w_f32, p.offset, c, p.d);
-        wp[j] = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
-        if (shared_gate) gs[j] = unpack8<false>(load8<false>(p.gate, c, p.d));
-      }
-      const V8 dy = unpack8<false>(cur.dy[j]), h = unpack8<kF32>(cur.h[j]), x = unpack8<false>(cur.x[j]),
-               dh = unpack8<kF32>(cur.dh[j]);
-      V8 o, dg, g;
-      if (p.gate != nullptr) g = shared_gate ? gs[j] : unpack8<false>(cur.g[j]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float hi = h.v[i], xi = x.v[i];
-        const float a0 = dy.v[i] * hi * rh;
-        const float dhi = fmaf(rh, fmaf(dy.v[i], wq[j].v[i], -hi * ch), dh.v[i]);
-        o.v[i] = p.res_scale * dhi;
-        const float xn = xi * rx;                                   // x, normalised if there is a norm
-        const float n = p.post ? xn * wp[j].v[i] : xn;
-        const float bd = p.branch_scale * dhi;
-        dg.v[i] = bd * n;
-        const float dn = p.gate == nullptr ? bd : bd * g.v[i];
-        const float a1 = dn * xn;
-        const float v = p.post ? dn * wp[j].v[i] : dn;
-        q[0] = fmaf(v, xi, q[0]);
-        vv[j].v[i] = v;
-        if (kHold) {
-          acc[0].v[i] += a0;
-          acc[1].v[i] += a1;
-          acc[2].v[i] += dg.v[i];
-        } else if (c + i < p.d) {
-          acc_smem[c + i] += a0;
-          acc_smem[p.d + c + i] += a1;
-          acc_smem[2 * p.d + c + i] += dg.v[i];
-        }
-      }
-      if (p.dres != nullptr)
-        store8<kF32>(static_cast<char*>(p.dres) + static_cast<size_t>(t) * p.lddres * es, c, p.d, o);
-      if (p.dgate != nullptr) store8<false>(p.dgate + static_cast<size_t>(t) * p.lddgate, c, p.d, dg);
-    }
-    if (p.dx == nullptr) continue;
-    float cx = 0.f;
+    float scale = p.branch_scale;
     if (p.post) {
-      block_sum<1>(q, red1[par]);
-      cx = rx * rx * q[0] * inv_d;
+      unsigned long long q = 0ull;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        const P8 x = pairs8<false>(cur.x[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q = fma2(x.p[i], x.p[i], q);
+      }
+      float s[1] = {sum2(q)};
+      block_sum<1>(s, red[2 * par]);
+      scale *= rsqrtf(fmaf(s[0], inv_d, p.eps));
     }
+    const unsigned long long scale2 = pair2(scale, scale), res2 = pair2(p.res_scale, p.res_scale);
+    unsigned long long q = 0ull;
+    P8 h[kVec];
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
       const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      const V8 x = unpack8<false>(cur.x[j]);
-      V8 o;
+      if (!kHold) gains(j);
+      const P8 x = pairs8<false>(cur.x[j]), r = pairs8<kF32>(cur.r[j]);
+      P8 w = wp[j];
+      if (token_gate) {
+        const P8 g = pairs8<false>(cur.g[j]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o.v[i] = rx * fmaf(-x.v[i], cx, vv[j].v[i]);
-      store8<false>(p.dx + static_cast<size_t>(t) * p.lddx, c, p.d, o);
-    }
-  }
-  grid_launch_dependents();
-  if (p.want == 0) return;
-  float* part = p.part + static_cast<size_t>(blockIdx.x) * 3 * p.d;
-#pragma unroll
-  for (int a = 0; a < 3; ++a) {
-    if (((p.want >> a) & 1) == 0) continue;
-    if (kHold) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int c = 8 * threadIdx.x + i;
-        if (c < p.d) part[static_cast<size_t>(a) * p.d + c] = acc[a].v[i];
+        for (int i = 0; i < 4; ++i) w.p[i] = mul2(w.p[i], g.p[i]);
       }
-    } else {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        for (int i = 0; i < 8; ++i) {
-          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
-          if (c < p.d) part[static_cast<size_t>(a) * p.d + c] = acc_smem[a * p.d + c];
-        }
+      for (int i = 0; i < 4; ++i) {
+        const unsigned long long b = mul2(mul2(x.p[i], scale2), w.p[i]);
+        h[j].p[i] = fma2(res2, r.p[i], b);
+        q = fma2(h[j].p[i], h[j].p[i], q);
+      }
+      if (p.h != nullptr) store8<kF32>(static_cast<char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, p.d, h[j]);
+    }
+    if (p.y == nullptr) continue;
+    float s[1] = {sum2(q)};
+    block_sum<1>(s, red[2 * par + 1]);
+    const float rh = rsqrtf(fmaf(s[0], inv_d, p.eps));
+    const unsigned long long rh2 = pair2(rh, rh);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+      P8 o;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o.p[i] = mul2(mul2(h[j].p[i], rh2), wq[j].p[i]);
+      store8<false>(p.y + static_cast<size_t>(t) * p.ldy, c, p.d, o);
     }
   }
 }
 
-// out_a[c] = sum over `rows` partial rows, in a fixed order: 16 interleaved runs, then the runs.
-__global__ void __launch_bounds__(512) column_sum_kernel(const float* __restrict__ part, int rows, long long row_stride,
-                                                        long long array_stride, int d, float* out0, float* out1,
-                                                        float* out2) {
-  __shared__ float s[16][33];
-  float* out = blockIdx.y == 0 ? out0 : (blockIdx.y == 1 ? out1 : out2);
-  const int lane = threadIdx.x & 31, run = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + lane;
+// Backward.  With G = b gate gain_post, v = dh G, and the sums over rows behind the gains and a shared gate are
+// d_post = b gate S and d_gate = b gain_post S with the same S = sum_t dh x r_x (times the row's gate, if
+// every token has its own), so a column needs two sums and two gains: they stay in registers with kVec == 1
+// (80 registers, four CTAs of 192 threads per SM at d = 1536: enough warps to cover each other's reductions
+// and loads; with prefetched rows as well, three warps per scheduler waited for their own shuffles, and with
+// gains in shared memory that memory's pipe was the limit).  Otherwise the sums are in shared memory
+// (dynamic, [2][d]) and gains are re-read.
+// kFull: every operand and result exists, no per-token gate, d a multiple of 256 (no thread or vector is
+// partly outside the row): the same arithmetic without the tests for it.  With a bf16 stream rows then arrive
+// through a ring of kRing stages in shared memory (asynchronous copies, two rows ahead), so that loads are in
+// flight during the reductions without taking registers: T = 65,536, d = 1536 takes 198 us with it and 259 us
+// without.  With an fp32 stream the ring is slower (387 us against 315 us).
+template <bool kF32, int kVec, bool kFull, int kThreads, int kBlocks>
+__global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormParams p) {
+  __shared__ SumBuf<3> red3[2];
+  __shared__ SumBuf<1> red1[2];
+  extern __shared__ __align__(16) float dyn[];  // sums over rows, or the ring
+  constexpr bool kHold = kVec == 1;
+  constexpr int kRing = norm_cfg::kRing;
+  constexpr bool kRows = kFull && !kF32;  // rows arrive through the ring
+  constexpr size_t es = kF32 ? 4 : 2;
+  const int nt = blockDim.x;
+  const float inv_d = 1.f / static_cast<float>(p.d);
+  const bool shared_gate = p.gate != nullptr && p.ldg == 0, token_gate = !kFull && p.gate != nullptr && p.ldg != 0;
+  const bool have_y = kFull || p.dy != nullptr, have_dh = kFull || p.dh != nullptr, have_x = kFull || p.x != nullptr;
+  P8 acc[2];  // kHold: sums over this CTA's rows of dy h r_h and of dh x r_x
+  P8 held[2];  // kHold: gain of y, G
+#pragma unroll
+  for (int i = 0; i < 4; ++i) acc[0].p[i] = acc[1].p[i] = held[0].p[i] = held[1].p[i] = 0ull;
+  auto shared_gate8 = [&](int c) { return shared_gate ? unpack8<false>(load8<false>(p.gate, c, p.d)) : gain8(nullptr, 0, 0.f, c, p.d); };
+  // which: 0 = gain of y, 1 = G (without a per-token gate)
+  auto read_gain = [&](int which, int c) {
+    if (which == 0) return pack8(gain8(p.w_pre, p.w_f32, p.offset, c, p.d));
+    V8 w = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
+    const V8 g = shared_gate8(c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w.v[i] *= p.branch_scale * g.v[i];
+    return pack8(w);
+  };
+  auto gain = [&](int which, int j) {
+    return kHold ? held[which] : read_gain(which, 8 * (static_cast<int>(threadIdx.x) + j * nt));
+  };
+  clear_sums(red3, 2);
+  clear_sums(red1, 2);
+  grid_dependency_wait();
+  if (kHold) {
+    held[0] = read_gain(0, 8 * static_cast<int>(threadIdx.x));
+    held[1] = read_gain(1, 8 * static_cast<int>(threadIdx.x));
+  } else {
+    // every thread clears, adds to and reads back its own columns only: no barrier needed
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        for (int i = 0; i < 8; ++i) {
+          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
+          if (c < p.d) dyn[a * p.d + c] = 0.f;
+        }
+  }
+  __syncthreads();
+  struct Row {
+    Raw8<false> dy[kVec], x[kVec], g[kVec];
+    Raw8<kF32> h[kVec], dh[kVec];
+  };
+  const int d_ = kFull ? 1 << 30 : p.d;  // kFull: no vector reaches past the row
+  auto fetch = [&](int t) {
+    Row o;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+      if (have_y) {
+        o.dy[j] = load8<false>(p.dy + static_cast<size_t>(t) * p.lddy, c, d_);
+        o.h[j] = load8<kF32>(static_cast<const char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, d_);
+      } else {
+        o.dy[j] = zero8<false>();
+        o.h[j] = zero8<kF32>();
+      }
+      o.dh[j] = have_dh ? load8<kF32>(static_cast<const char*>(p.dh) + static_cast<size_t>(t) * p.lddh * es, c, d_) : zero8<kF32>();
+      o.x[j] = have_x ? load8<false>(p.x + static_cast<size_t>(t) * p.ldx, c, d_) : zero8<false>();
+      if (token_gate) o.g[j] = load8<false>(p.gate + static_cast<size_t>(t) * p.ldg, c, d_);
+    }
+    return o;
+  };
+  // the ring: slots of a stage are dy, x, h, dh
+  constexpr int kSlots = 4;
+  const uint32_t slot = 16u * static_cast<uint32_t>(nt), ring0 = smem_u32(dyn) + 16u * threadIdx.x;
+  auto issue = [&](int t, int stage) {
+    if (t < p.T) {
+      const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
+      async_copy16(at, p.dy + static_cast<size_t>(t) * p.lddy + 8 * threadIdx.x);
+      async_copy16(at + slot, p.x + static_cast<size_t>(t) * p.ldx + 8 * threadIdx.x);
+      async_copy16(at + 2 * slot, static_cast<const __nv_bfloat16*>(p.h) + static_cast<size_t>(t) * p.ldh + 8 * threadIdx.x);
+      async_copy16(at + 3 * slot, static_cast<const __nv_bfloat16*>(p.dh) + static_cast<size_t>(t) * p.lddh + 8 * threadIdx.x);
+    }
+    async_commit();
+  };
+  auto take = [&](int stage) {
+    Row o;
+    const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
+    o.dy[0].q[0] = ring_get(at);
+    o.x[0].q[0] = ring_get(at + slot);
+    o.h[0].q[0] = ring_get(at + 2 * slot);
+    o.dh[0].q[0] = ring_get(at + 3 * slot);
+    return o;
+  };
+  const unsigned long long rs2 = pair2(p.res_scale, p.res_scale);
+  int par = 0, stage = 0;
+  if (kRows)
+    for (int i = 0; i < kRing; ++i) issue(blockIdx.x + i * static_cast<int>(gridDim.x), i);
+  for (int t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+    Row cur;
+    if (kRows) {
+      async_wait<kRing - 1>();
+      cur = take(stage);
+    } else {
+      cur = fetch(t);
+    }
+    P8 vv[kVec];
+    unsigned long long s0 = 0ull, s1 = 0ull, s2 = 0ull;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const P8 dy = pairs8<false>(cur.dy[j]), h = pairs8<kF32>(cur.h[j]), x = pairs8<false>(cur.x[j]), wq = gain(0, j);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s0 = fma2(h.p[i], h.p[i], s0);
+        s1 = fma2(mul2(dy.p[i], wq.p[i]), h.p[i], s1);
+        s2 = fma2(x.p[i], x.p[i], s2);
+      }
+    }
+    if (kRows) {
+      // the stage's values are in registers: its place is free for the row kRing further on
+      issue(t + kRing * static_cast<int>(gridDim.x), stage);
+      stage = stage + 1 == kRing ? 0 : stage + 1;
+    }
+    float s[3] = {sum2(s0), sum2(s1), sum2(s2)};  // sum h^2, sum g h, sum x^2
+    block_sum<3>(s, red3[par]);
+    const float rh = have_y ? rsqrtf(fmaf(s[0], inv_d, p.eps)) : 0.f;
+    const float rx = p.post ? rsqrtf(fmaf(s[2], inv_d, p.eps)) : 1.f;
+    const float ch = -rh * rh * s[1] * inv_d;
+    const unsigned long long rh2 = pair2(rh, rh), ch2 = pair2(ch, ch), rx2 = pair2(rx, rx);
+    unsigned long long q = 0ull;  // sum v x
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+      const P8 dy = pairs8<false>(cur.dy[j]), h = pairs8<kF32>(cur.h[j]), x = pairs8<false>(cur.x[j]),
+               dh = pairs8<kF32>(cur.dh[j]);
+      const P8 wq = gain(0, j), G = gain(1, j);
+      P8 o, dg, g;
+      if (token_gate) g = pairs8<false>(cur.g[j]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned long long d2 = fma2(rh2, fma2(h.p[i], ch2, mul2(dy.p[i], wq.p[i])), dh.p[i]);  // dh
+        o.p[i] = mul2(rs2, d2);
+        unsigned long long xn = mul2(x.p[i], rx2);  // x, normalised if there is a norm
+        unsigned long long v = mul2(d2, G.p[i]);
+        if (token_gate) {
+          dg.p[i] = mul2(v, xn);
+          v = mul2(v, g.p[i]);
+          xn = mul2(xn, g.p[i]);
+        }
+        q = fma2(v, x.p[i], q);
+        vv[j].p[i] = v;
+        if (kHold) {
+          acc[0].p[i] = fma2(mul2(dy.p[i], h.p[i]), rh2, acc[0].p[i]);
+          acc[1].p[i] = fma2(d2, xn, acc[1].p[i]);
+        } else {
+          const float2 b0 = unpair2(mul2(mul2(dy.p[i], h.p[i]), rh2)), b1 = unpair2(mul2(d2, xn));
+          const int e = c + 2 * i;
+          if (e < p.d) {
+            dyn[e] += b0.x;
+            dyn[p.d + e] += b1.x;
+          }
+          if (e + 1 < p.d) {
+            dyn[e + 1] += b0.y;
+            dyn[p.d + e + 1] += b1.y;
+          }
+        }
+      }
+      if (kFull || p.dres != nullptr)
+        store8<kF32>(static_cast<char*>(p.dres) + static_cast<size_t>(t) * p.lddres * es, c, d_, o);
+      if (token_gate && p.dgate != nullptr) store8<false>(p.dgate + static_cast<size_t>(t) * p.lddgate, c, d_, dg);
+    }
+    if (!kFull && p.dx == nullptr) continue;
+    if (p.post) {
+      float sq[1] = {sum2(q)};
+      block_sum<1>(sq, red1[par]);
+      const float cx = -rx * rx * sq[0] * inv_d;
+      const unsigned long long cx2 = pair2(cx, cx);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        const P8 x = pairs8<false>(cur.x[j]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vv[j].p[i] = mul2(rx2, fma2(x.p[i], cx2, vv[j].p[i]));
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      store8<false>(p.dx + static_cast<size_t>(t) * p.lddx, 8 * (static_cast<int>(threadIdx.x) + j * nt), d_, vv[j]);
+  }
+  grid_launch_dependents();
+  if (p.want == 0) return;
+  float* part = p.part + static_cast<size_t>(blockIdx.x) * 2 * p.part_d;
+  if (kHold) {
+    // rows of part_d floats: 16-byte stores; columns beyond d hold zeros
+    const int c = 8 * threadIdx.x;
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        if (c + 2 * i < p.part_d)
+          *reinterpret_cast<ulonglong2*>(part + static_cast<size_t>(a) * p.part_d + c + 2 * i) = make_ulonglong2(acc[a].p[i], acc[a].p[i + 1]);
+  } else {
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        for (int i = 0; i < 8; ++i) {
+          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
+          if (c < p.part_d) part[static_cast<size_t>(a) * p.part_d + c] = c < p.d ? dyn[a * p.d + c] : 0.f;
+        }
+  }
+}
+
+// Sums of 32 columns from c0 on over `rows` rows of `part` (row_stride floats apart, a multiple of 4, 16-byte
+// aligned, readable up to a multiple of 4 columns), in a fixed order: 128 interleaved runs of four columns per
+// thread, all of a thread's loads in flight together, then the runs.  Block of 1024; warp w returns column c0 + w
+// in every lane.
+__device__ __forceinline__ float column_total(const float* part, int rows, long long row_stride, int c0, int d) {
+  __shared__ float s[128][33];
+  const int quad = threadIdx.x & 7, run = threadIdx.x >> 3;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (c0 + 4 * quad < d) {
+    const float* q = part + c0 + 4 * quad;
+#pragma unroll 8
+    for (int r = run; r < rows; r += 128) {
+      const float4 u = *reinterpret_cast<const float4*>(q + static_cast<size_t>(r) * row_stride);
+      v.x += u.x;
+      v.y += u.y;
+      v.z += u.z;
+      v.w += u.w;
+    }
+  }
+  s[run][4 * quad] = v.x;
+  s[run][4 * quad + 1] = v.y;
+  s[run][4 * quad + 2] = v.z;
+  s[run][4 * quad + 3] = v.w;
+  __syncthreads();
+  const int lane = threadIdx.x & 31, col = threadIdx.x >> 5;
+  return warp_sum((s[lane][col] + s[lane + 32][col]) + (s[lane + 64][col] + s[lane + 96][col]));
+}
+
+// The gradients of the gains and of a shared gate from the partial sums: blockIdx.y 0: d_pre, 1: d_post and d_gate.
+__global__ void __launch_bounds__(1024) norm_sums_kernel(const NormParams p, int rows, float* d_pre, float* d_post, float* d_gate) {
   grid_dependency_wait();
   grid_launch_dependents();
-  if (out == nullptr) return;
-  float v = 0.f;
-  if (c < d) {
-    const float* q = part + blockIdx.y * array_stride + c;
-#pragma unroll 4
-    for (int r = run; r < rows; r += 16) v += q[static_cast<size_t>(r) * row_stride];
+  if (blockIdx.y == 0 ? d_pre == nullptr : (d_post == nullptr && d_gate == nullptr)) return;
+  const int c0 = blockIdx.x * 32, c = c0 + (static_cast<int>(threadIdx.x) >> 5);
+  const float t = column_total(p.part + static_cast<size_t>(blockIdx.y) * p.part_d, rows, 2ll * p.part_d, c0, p.d);
+  if ((threadIdx.x & 31) != 0 || c >= p.d) return;
+  if (blockIdx.y == 0) {
+    d_pre[c] = t;
+    return;
   }
-  s[run][lane] = v;
-  __syncthreads();
-  if (run == 0 && c < d) {
-    float t = 0.f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) t += s[k][lane];
-    out[c] = t;
+  // S -> b gate S and b gain_post S (a per-token gate is already in S)
+  const float gate = p.gate != nullptr && p.ldg == 0 ? __bfloat162float(p.gate[c]) : 1.f;
+  if (d_post != nullptr) d_post[c] = p.branch_scale * gate * t;
+  if (d_gate != nullptr) {
+    float w = 1.f;
+    if (p.w_post != nullptr)
+      w = (p.w_f32 ? static_cast<const float*>(p.w_post)[c] : __bfloat162float(static_cast<const __nv_bfloat16*>(p.w_post)[c])) + p.offset;
+    d_gate[c] = p.branch_scale * w * t;
   }
+}
+
+// out[c] = sum over `rows` partial rows of row_stride (a multiple of 4) floats.
+__global__ void __launch_bounds__(1024) column_sum_kernel(const float* __restrict__ part, int rows, long long row_stride, int d, float* out) {
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int c0 = blockIdx.x * 32, c = c0 + (static_cast<int>(threadIdx.x) >> 5);
+  const float t = column_total(part, rows, row_stride, c0, d);
+  if ((threadIdx.x & 31) == 0 && c < d) out[c] = t;
 }
 
 }  // namespace npd
