@@ -411,7 +411,7 @@ def _new(shape, dtype, device):
     cols = shape[1]
     if cols % 8 == 0:
         return torch.empty(shape, dtype=dtype, device=device)
-    return torch.empty((shape[0], (cols + 7) // 8 * 8), dtype=dtype, device=device)[:, :cols]
+    return torch.empty_strided(shape, ((cols + 7) // 8 * 8, 1), dtype=dtype, device=device)
 
 
 def _like(t, shape, dtype):

@@ -13,7 +13,7 @@ LIB_PATH = os.path.join(HERE, "libnpd.so")
 SOURCES = [os.path.join(HERE, "csrc", "npd_api.cu")]
 DEPS = [os.path.join(HERE, "csrc", f) for f in
         ("npd_api.cu", "ptx_sm100.cuh", "gemm_sm100.cuh", "kd_tile_sm100.cuh", "small_kernels.cuh",
-         "norm_kernels.cuh", "norm_api.cuh", "pair_tile_sm100.cuh", "ce_kernels.cuh", "ce_api.cuh",
+         "norm_kernels.cuh", "norm_api.cuh", "pair_tile_sm100.cuh", "rows_sm100.cuh", "ce_kernels.cuh", "ce_api.cuh",
          "linear_kernels.cuh", "linear_api.cuh")]
 DEPS.append(os.path.join(os.path.dirname(HERE), "include", "npd.h"))
 

@@ -17,8 +17,8 @@ CePlan ce_plan(const npd_ce_args* a, int sms) {
   pl.vtiles = (a->V + 255) / 256;
   pl.clusters = std::max(sms / 2, 1);
   // As many runs as CTA pairs: a batch of one pair of row blocks (a few tokens to score) then still
-  // keeps every SM reading its own part of the weights.  The partials cost 32 bytes per token and run.
-  pl.nsplit_max = std::min(pl.vtiles, pl.clusters);
+  // has every SM reading its own part of the weights.  The partials cost 32 bytes per token and run.
+  pl.nsplit_max = std::min({pl.vtiles, pl.clusters, 127});
   pl.grads = a->d_hidden != nullptr || a->d_weight != nullptr;
   // Pieces of the vocabulary in the backward: by default the widest whose bf16 gradient block stays
   // within 256 MiB or a sixteenth of what bf16 logits would take, whichever is more, all of (almost) equal width.
@@ -44,7 +44,7 @@ CePlan ce_plan(const npd_ce_args* a, int sms) {
   pl.off_cy = take(sizeof(int) * crows);
   pl.off_cw = take(sizeof(float) * crows);
   pl.off_hc = take(2 * crows * a->d);
-  pl.off_partials = take(sizeof(float2) * 4 * pl.nsplit_max * crows);
+  pl.off_partials = take(sizeof(float2) * std::max(4 * pl.nsplit_max, a->T <= ce_rows_cfg::kTokens ? 3 * sms : 0) * crows);
   pl.off_zlabel = take(sizeof(float) * crows);
   pl.off_zy = take(sizeof(float) * crows);
   pl.off_lse2 = take(sizeof(float) * crows);
@@ -140,7 +140,8 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
   __nv_bfloat16* hc = reinterpret_cast<__nv_bfloat16*>(ws + pl.off_hc);
   float* dh_acc = a->d_hidden != nullptr ? reinterpret_cast<float*>(ws + pl.off_dh) : nullptr;
   CUtensorMap mh, mw;
-  if (!make_map(&mh, hc, a->d, crows, a->d, 64, 128) || !make_map(&mw, a->weight, a->d, a->V, a->ldw, 64, 128))
+  // the compact rows end at T at the latest: rows of a tile beyond it are filled with zeros without a fetch
+  if (!make_map(&mh, hc, a->d, a->T, a->d, 64, 128) || !make_map(&mw, a->weight, a->d, a->V, a->ldw, 64, 128))
     return NPD_ECUDA;
 
   CePlanParams pp{};
@@ -166,7 +167,10 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
   pp.hc = hc;
   pp.dh_acc = dh_acc;
   pp.status = status;
-  if (launch_ex(ce_plan_kernel, std::min(di.sms, (a->T + 7) / 8), 1024, 0, st, false, pp) != cudaSuccess) return NPD_ECUDA;
+  pp.pad = pl.grads ? 1 : 0;
+  // eight tokens per block or more; with rows to be cleared at least as many blocks as make that quick
+  const int plan_blocks = std::min(di.sms, std::max((a->T + 7) / 8, pl.grads ? 4 : 1));
+  if (launch_ex(ce_plan_kernel, plan_blocks, 1024, 0, st, false, pp) != cudaSuccess) return NPD_ECUDA;
   ++g_launches;
 
   CeTileParams tp{};
@@ -184,10 +188,39 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
   tp.zlabel = reinterpret_cast<float*>(ws + pl.off_zlabel);
   tp.lse2 = reinterpret_cast<float*>(ws + pl.off_lse2);
   tp.status = status;
-  if ((rc = launch_pair_tile<CeForwardEpi>(mh, mw, tp, pl.clusters, st, pdl)) != NPD_OK) return rc;
+  int slots = 0;
+  const int rows_smem = 2 * ce_rows_cfg::kTokens * a->d;
+  if (a->T <= ce_rows_cfg::kTokens && rows_smem <= ce_rows_cfg::kMaxTokenBytes) {
+    CeRowsParams rp{};
+    rp.V = a->V;
+    rp.d = a->d;
+    rp.plan = pp.plan;
+    rp.cy = pp.cy;
+    rp.hc = hc;
+    rp.weight = pp.head;
+    rp.ldw = a->ldw;
+    rp.rows = tp.rows;
+    rp.scale2 = tp.scale2;
+    rp.partials = tp.partials;
+    rp.zlabel = tp.zlabel;
+    // Batches of loads that divide a warp's share of K waste none: 3 steps where the share is a multiple of 3 and not of
+    // 4 (d = 1536: 6), else 4.  Smaller batches leave registers for a third block per SM.
+    const int share = (a->d / 32 + ce_rows_cfg::kWarps - 1) / ce_rows_cfg::kWarps;
+    const bool three = share % 3 == 0 && share % 4 != 0 && rows_smem <= 48 * 1024;
+    // as many blocks as are resident, as far as there are groups of 16 rows (the workspace has room for three per SM)
+    slots = std::max(1, std::min({(three ? 3 : 2) * di.sms, (a->V + 15) / 16}));
+    auto k = three ? ce_rows_kernel<3> : ce_rows_kernel<4>;
+    if (set_smem(k, ce_rows_cfg::kMaxTokenBytes) != NPD_OK) return NPD_ECUDA;
+    const cudaError_t e = launch_ex(k, slots, ce_rows_cfg::kThreads, rows_smem, st, pdl, rp);
+    ++g_launches;
+    if (e != cudaSuccess) return NPD_ECUDA;
+  } else if ((rc = launch_pair_tile<CeForwardEpi>(mh, mw, tp, pl.clusters, st, pdl)) != NPD_OK) {
+    return rc;
+  }
 
   CeMergeParams mp{};
   mp.T = a->T;
+  mp.slots = slots;
   mp.plan = pp.plan;
   mp.cidx = pp.cidx;
   mp.partials = tp.partials;
@@ -197,7 +230,9 @@ int npd_ce_fwd_bwd(const npd_ce_args* a, void* cuda_stream) {
   mp.nll = a->nll;
   mp.lse = a->lse;
   mp.lse2 = reinterpret_cast<float*>(ws + pl.off_lse2);
-  if (launch_ex(ce_merge_kernel, (a->T + 31) / 32, 256, 0, st, pdl, mp) != cudaSuccess) return NPD_ECUDA;
+  if ((slots > 0 ? launch_ex(ce_merge_rows_kernel, a->T, 256, 0, st, pdl, mp)
+                 : launch_ex(ce_merge_kernel, (a->T + 31) / 32, 256, 0, st, pdl, mp)) != cudaSuccess)
+    return NPD_ECUDA;
   ++g_launches;
   if (!pl.grads) return NPD_OK;
 

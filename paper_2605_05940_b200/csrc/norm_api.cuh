@@ -179,7 +179,7 @@ template <bool kF32>
 void (*norm_bwd_pick(const NormPlan& pl, bool full))(NormParams) {
   if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, false, 512, 1>;
   if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, false, 512, 1>;
-  if (pl.threads <= 256) return full ? norm_bwd_kernel<kF32, 1, true, 256, 3> : norm_bwd_kernel<kF32, 1, false, 256, 3>;
+  if (pl.threads <= 256) return full ? norm_bwd_kernel<kF32, 1, true, 256, 3> : norm_bwd_kernel<kF32, 1, false, 256, 2>;
   return full ? norm_bwd_kernel<kF32, 1, true, 512, 1> : norm_bwd_kernel<kF32, 1, false, 512, 1>;
 }
 
@@ -235,14 +235,16 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   const bool full = pl.vec == 1 && a->d % 256 == 0 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr &&
                     p.dres != nullptr && (p.gate == nullptr || p.ldg == 0);
   auto k = sf ? norm_bwd_pick<true>(pl, full) : norm_bwd_pick<false>(pl, full);
+  // without the full form's registers fewer CTAs are resident (the workspace is sized for the larger number)
+  const int grid = full ? pl.grid : std::min(pl.grid, di.sms * std::max(1, 512 / pl.threads));
   const int smem = full && !sf ? norm_cfg::kRing * pl.threads * 16 * 4 : pl.smem;
   if (smem > 0 && set_smem(k, norm_cfg::kMaxSmem) != NPD_OK) return NPD_ECUDA;
-  cudaError_t e = launch_ex(k, pl.grid, pl.threads, smem, st, false, p);
+  cudaError_t e = launch_ex(k, grid, pl.threads, smem, st, false, p);
   ++g_launches;
   if (e != cudaSuccess) return NPD_ECUDA;
   if (p.want != 0) {
     float* shared_dgate = (p.want & 4) ? static_cast<float*>(a->d_gate) : nullptr;
-    e = launch_dim(norm_sums_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 2), 1024, 0, st, true, p, pl.grid,
+    e = launch_dim(norm_sums_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 2), 1024, 0, st, true, p, grid,
                    a->d_pre_weight, a->d_post_weight, shared_dgate);
     ++g_launches;
   }
