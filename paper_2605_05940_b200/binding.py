@@ -503,11 +503,11 @@ def npd_norm_fwd(x, residual=None, *, gate=None, post_weight=None, pre_weight=No
 
 def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_weight=None, post_norm=False, eps=1e-6,
                  weight_offset=0.0, residual_scale=1.0, branch_scale=1.0, want_dresidual=True, want_dweights=True,
-                 dx=None, dresidual=None, workspace=None, stream=None):
+                 dx=None, dresidual=None, d_post_weight=None, d_pre_weight=None, d_gate=None, workspace=None, stream=None):
     """Gradients of npd_norm_fwd.  dy is the gradient at y (or None), h the forward's h, dh the gradient that
     arrives at h from elsewhere (or None); the rest as in the forward.  Returns (dx, dresidual,
-    d_post_weight, d_pre_weight, d_gate), None for what has no counterpart in the call; the gradients of
-    the gains and of a shared gate are f32 [d] sums over the tokens."""
+    d_post_weight, d_pre_weight, d_gate) in the tensors given or in new ones, None for what has no counterpart in
+    the call; the gradients of the gains and of a shared gate are f32 [d] sums over the tokens."""
     where = "npd_norm_bwd"
     first = dy if dy is not None else dh
     dev = _device_of(first, where)
@@ -534,21 +534,24 @@ def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_wei
             a.lddx, a.dx = _matrix(dx, where, dev, shape, bf16), dx.data_ptr()
         if dresidual is not None:
             a.lddr, a.dresidual = _matrix(dresidual, where, dev, shape, sd), dresidual.data_ptr()
-        d_post = d_pre = d_gate = None
-        if want_dweights and post_norm and post_weight is not None:
+        d_post, d_pre = d_post_weight, d_pre_weight
+        if d_post is None and want_dweights and post_norm and post_weight is not None:
             d_post = torch.empty(d, dtype=torch.float32, device=device)
-            a.d_post_weight = d_post.data_ptr()
-        if want_dweights and pre_weight is not None and dy is not None:
+        if d_pre is None and want_dweights and pre_weight is not None and dy is not None:
             d_pre = torch.empty(d, dtype=torch.float32, device=device)
-            a.d_pre_weight = d_pre.data_ptr()
+        a.d_post_weight = _vector(d_post, where, dev, d, torch.float32)
+        a.d_pre_weight = _vector(d_pre, where, dev, d, torch.float32)
         shared = gate is not None and gate.dim() == 1
-        if gate is not None:
-            if shared:
+        if shared:
+            if d_gate is None:
                 d_gate = torch.empty(d, dtype=torch.float32, device=device)
-            else:
+            a.d_gate = _vector(d_gate, where, dev, d, torch.float32)
+        elif gate is not None:
+            if d_gate is None:
                 d_gate = _new(shape, bf16, device)
-                a.lddg = _matrix(d_gate, where, dev, shape, bf16)
-            a.d_gate = d_gate.data_ptr()
+            a.lddg, a.d_gate = _matrix(d_gate, where, dev, shape, bf16), d_gate.data_ptr()
+        elif d_gate is not None:
+            raise NpdError(NPD_EINVAL, where)
         if d_post is not None or d_pre is not None or shared:
             if workspace is None:
                 n = C.c_size_t(0)
@@ -643,18 +646,66 @@ def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_
     return dx, dw, dbias
 
 
+class NormJoin:
+    """What stands between a student's last block and its LM head: h = residual_scale * residual +
+    branch_scale * gate * (norm of x, or x), hidden states = norm of h (npd_norm_fwd / npd_norm_bwd), with its
+    buffers.  Given to KDStep or CEStep as `norm`, every run of the step first writes the step's hidden states and
+    afterwards turns their gradient into those of x, residual, gate and gains: dx, dresidual, d_post_weight,
+    d_pre_weight, d_gate.  Arguments as for npd_norm_fwd."""
+
+    def __init__(self, x, residual=None, *, grads=True, **how):
+        self.x, self.residual, self.how, self.grads = x, residual, how, grads
+        first = x if x is not None else residual
+        dev = _device_of(first, "NormJoin")
+        shape, device = first.shape, first.device
+        if len(shape) != 2:
+            raise NpdError(NPD_ESHAPE, "NormJoin")
+        with _scope(dev, None):
+            sd = residual.dtype if residual is not None else torch.bfloat16
+            self.h = _new(shape, sd, device)
+            self.dx = self.dresidual = self.d_post_weight = self.d_pre_weight = self.d_gate = None
+            if not grads:
+                return
+            d, gate = shape[1], how.get("gate")
+            f32 = lambda: torch.empty(d, dtype=torch.float32, device=device)
+            if x is not None:
+                self.dx = _new(shape, torch.bfloat16, device)
+            if residual is not None:
+                self.dresidual = _new(shape, sd, device)
+            if how.get("post_norm") and how.get("post_weight") is not None:
+                self.d_post_weight = f32()
+            if how.get("pre_weight") is not None:
+                self.d_pre_weight = f32()
+            if gate is not None:
+                self.d_gate = f32() if gate.dim() == 1 else _new(shape, torch.bfloat16, device)
+            a = npd_norm_args(C.sizeof(npd_norm_args), shape[0], d, _DT[sd])
+            n = C.c_size_t(0)
+            _check(lib().npd_norm_workspace_bytes(a, n), "npd_norm_workspace_bytes")
+            self._workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
+
+    def forward(self, hidden, stream=None):
+        npd_norm_fwd(self.x, self.residual, h=self.h, y=hidden, stream=stream, **self.how)
+
+    def backward(self, d_hidden, stream=None):
+        npd_norm_bwd(d_hidden, self.h, self.x, dx=self.dx, dresidual=self.dresidual, want_dresidual=False,
+                     d_post_weight=self.d_post_weight, d_pre_weight=self.d_pre_weight, d_gate=self.d_gate,
+                     workspace=self._workspace, stream=stream, **self.how)
+
+
 class CEStep:
     """Cross-entropy of the LM head for one set of tensors: checks them, holds the results (nll, lse,
     d_hidden, d_weight) and the workspace, and runs the step on them; see npd_ce_args in include/npd.h.
 
     hidden bf16 [T, d], weight bf16 [V, d], labels int32 [T], loss_mask uint8 or bool [T], token_weight f32 [T].
+    norm: a NormJoin that writes `hidden` before, and takes d_hidden back after the step.
     d_hidden / d_weight: True for a new tensor, None for none, or a tensor to write to (an f32 d_weight with
     accumulate_dw is added to).  The tensors are allocated on `stream` (default: the current one)."""
 
     def __init__(self, hidden, weight, labels, *, loss_mask=None, token_weight=None, temperature=1.0, grad_scale=1.0,
                  d_hidden=True, d_weight=True, dw_dtype=torch.bfloat16, accumulate_dw=False, want_lse=True,
-                 grad_chunk_cols=0, flags=0, workspace=None, stream=None):
+                 grad_chunk_cols=0, flags=0, workspace=None, norm=None, stream=None):
         where = "npd_ce_fwd_bwd"
+        self.norm = norm
         dev = self._dev = _device_of(hidden, where)
         if hidden.dim() != 2 or weight.dim() != 2:
             raise NpdError(NPD_ESHAPE, where)
@@ -698,8 +749,12 @@ class CEStep:
 
     def run(self, stream=None):
         """Enqueues the step on `stream` (default: the current one of the tensors' GPU)."""
+        if self.norm is not None:
+            self.norm.forward(self._inputs[0], stream)
         with _scope(self._dev, stream):
             _check(lib().npd_ce_fwd_bwd(self.args, _current(self._dev)), "npd_ce_fwd_bwd")
+        if self.norm is not None and self.d_hidden is not None and self.norm.grads:
+            self.norm.backward(self.d_hidden, stream)
 
     def status(self, stream=None) -> int:
         """Waits for `stream` and returns the status that the step's kernels left in the workspace."""
@@ -724,7 +779,8 @@ class KDStep:
     fused step on them; a convenience over the raw calls."""
 
     def __init__(self, batch, *, grads=True, dw_dtype=torch.bfloat16, grad_chunk_cols=0, grad_scale=None,
-                 kd_lambda=None, topk_values=None, topk_indices=None, flags=0):
+                 kd_lambda=None, topk_values=None, topk_indices=None, flags=0, norm=None):
+        self.norm = norm   # a NormJoin that writes batch.hidden before, and takes d_hidden back after the step
         dev = batch.hidden.device
         T, d, V = batch.T, batch.d, batch.V
         f32 = dict(dtype=torch.float32, device=dev)
@@ -755,7 +811,11 @@ class KDStep:
                                  **self._kw)
 
     def run(self, stream=None):
+        if self.norm is not None:
+            self.norm.forward(self.batch.hidden, stream)
         npd_kd_fwd_bwd(self.args, stream)
+        if self.norm is not None and self.d_hidden is not None and self.norm.grads:
+            self.norm.backward(self.d_hidden, stream)
 
     def phase_names(self):
         """Names of the launch groups of a call, in the order their phase events are recorded."""
