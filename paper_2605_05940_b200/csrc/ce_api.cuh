@@ -100,10 +100,10 @@ int check_ce(const npd_ce_args* a, bool need_pointers) {
 template <class Epi>
 int launch_pair_tile(const CUtensorMap& ma, const CUtensorMap& mb, const typename Epi::Params& p, int pairs, cudaStream_t st,
                      bool pdl) {
-  using namespace pair_cfg;
+  using L = PairCfg<Epi::kBN>;
   auto k = pair_tile_kernel<Epi>;
-  if (set_smem(k, SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
-  const cudaError_t e = launch_ex(k, 2 * pairs, THREADS, SMEM_BYTES, st, pdl, ma, mb, p);
+  if (set_smem(k, L::SMEM_BYTES) != NPD_OK) return NPD_ECUDA;
+  const cudaError_t e = launch_ex(k, 2 * pairs, L::THREADS, L::SMEM_BYTES, st, pdl, ma, mb, p);
   ++g_launches;
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;
 }

@@ -217,6 +217,8 @@ struct CeWalk {
 struct CeForwardEpi {
   using Params = CeTileParams;
   using Walk = CeWalk<true>;
+  static constexpr int kBN = 256;
+  static __device__ __forceinline__ int rows(const Params& p) { return 128 * p.plan[0]; }
   const Params& p;
   int pair_row, quarter, row, y, tc;
   float m, s;
@@ -337,19 +339,22 @@ __global__ void __launch_bounds__(ce_rows_cfg::kThreads, kBatch == 3 ? 3 : 2) ce
 struct CeGradientEpi {
   using Params = CeTileParams;
   using Walk = CeWalk<false>;
+  static constexpr int kBN = 256;
+  static __device__ __forceinline__ int rows(const Params& p) { return 128 * p.plan[0]; }
   const Params& p;
   int pair_row, tc, blocks128, y, row0;
+  bool on;
   float w, lse2;
   __device__ __forceinline__ CeGradientEpi(const Params& p_, int pair_row_, int)
-      : p(p_), pair_row(pair_row_), tc(p_.plan[3]), blocks128(128 * p_.plan[0]), y(-1), row0(-1), w(0.f), lse2(1e30f) {}
+      : p(p_), pair_row(pair_row_), tc(p_.plan[3]), blocks128(128 * p_.plan[0]), y(-1), row0(-1), on(false), w(0.f), lse2(1e30f) {}
   __device__ __forceinline__ void begin(const PairTile& t) {
     if (t.row0 == row0) return;
     row0 = t.row0;
     const int row = row0 + pair_row;
-    const bool on = row < tc;
+    on = row < tc;
     y = on ? p.cy[row] : -1;
     w = on ? p.cw[row] : 0.f;
-    lse2 = on ? p.lse2[row] : 1e30f;  // beyond the last row: p = 0, G = 0
+    lse2 = on ? p.lse2[row] : 0.f;
   }
   __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0) {
     if (row0 + pair_row >= blocks128) return;  // a block of rows that does not exist: nothing to store
@@ -363,10 +368,11 @@ struct CeGradientEpi {
         if (i == yi) g[i] = w * (ex2f(fmaf(__uint_as_float(acc[i]), p.scale2, -lse2)) - 1.f);
     }
     const int nvalid = p.V - col0;
-    if (nvalid < 32) {
+    // columns beyond V, and rows beyond the last token (whatever their logits), multiply real numbers: zeros
+    if (nvalid < 32 || !on) {
 #pragma unroll
       for (int i = 0; i < 32; ++i)
-        if (i >= nvalid) g[i] = 0.f;
+        if (i >= nvalid || !on) g[i] = 0.f;
     }
     store_row32<false>(p.gbuf + static_cast<size_t>(row0 + pair_row) * p.ldg + (col0 - p.g_col0), g, 32, true);
   }

@@ -97,15 +97,33 @@ cudaError_t launch_rows(const LinearParams& p, cudaStream_t st) {
   return launch_ex(linear_rows_kernel<kG>, (p.N + 15) / 16, 32 * rows_cfg::kWarps, 0, st, false, p);
 }
 
-template <bool kY32, bool kKeepZ>
-int launch_linear_tiles(const npd_linear_args* a, const LinearParams& p, int sms, cudaStream_t st) {
+template <bool kY32, bool kKeepZ, int kBN>
+int launch_linear_tiles_n(const npd_linear_args* a, LinearParams p, int sms, cudaStream_t st) {
   CUtensorMap mx, mw;
-  if (!make_map(&mx, a->x, a->K, a->M, a->ldx, 64, 128) || !make_map(&mw, a->weight, a->K, a->N, a->ldw, 64, 128))
+  if (!make_map(&mx, a->x, a->K, a->M, a->ldx, 64, 128) || !make_map(&mw, a->weight, a->K, a->N, a->ldw, 64, kBN / 2))
     return NPD_ECUDA;
+  p.ntiles = (a->N + kBN - 1) / kBN;
   const int pairs = std::max(1, std::min(p.mtiles * p.ntiles, sms / 2));
-  return launch_pair_tile<LinearEpi<kY32, kKeepZ>>(mx, mw, p, pairs, st, false);
+  return launch_pair_tile<LinearEpi<kY32, kKeepZ, kBN>>(mx, mw, p, pairs, st, false);
 }
 
+// Width of the tiles: the narrowest whose number still fits one round of the CTA pairs, so that a small problem
+// spreads over more of them, else 256 (a wide tile feeds the tensor cores better).  Measured at K = 4096, N = 4096, 256 /
+// 128 / 64 wide: M = 256 32.1 / 25.0 / 23.9 us (16, 32, 64 tiles), M = 512 32.8 / 26.0 / 40.8, M = 1024 34.1 / 43.8 / 74.4.
+int linear_tile_width(int M, int N, int pairs) {
+  const long long rows = (M + 255) / 256;
+  for (int bn : {64, 128})
+    if (rows * ((N + bn - 1) / bn) <= pairs) return bn;
+  return 256;
+}
+
+template <bool kY32, bool kKeepZ>
+int launch_linear_tiles(const npd_linear_args* a, const LinearParams& p, int sms, cudaStream_t st) {
+  const int bn = linear_tile_width(a->M, a->N, std::max(1, sms / 2));
+  if (bn == 256) return launch_linear_tiles_n<kY32, kKeepZ, 256>(a, p, sms, st);
+  if (bn == 128) return launch_linear_tiles_n<kY32, kKeepZ, 128>(a, p, sms, st);
+  return launch_linear_tiles_n<kY32, kKeepZ, 64>(a, p, sms, st);
+}
 }  // namespace
 
 extern "C" {
@@ -150,7 +168,6 @@ int npd_linear_fwd(const npd_linear_args* a, void* cuda_stream) {
     return e == cudaSuccess ? NPD_OK : NPD_ECUDA;
   }
   p.mtiles = (a->M + 255) / 256;
-  p.ntiles = (a->N + 255) / 256;
   p.group = static_cast<int>(std::max<long long>(4, (32ll << 20) / (512ll * a->K)));
   if (p.y_f32)
     return p.z != nullptr ? launch_linear_tiles<true, true>(a, p, di.sms, st) : launch_linear_tiles<true, false>(a, p, di.sms, st);

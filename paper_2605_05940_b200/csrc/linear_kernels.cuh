@@ -85,7 +85,7 @@ struct LinearParams {
   long long ldy, ldz;
   int y_f32;                    // linear_rows_kernel only: y and residual are fp32
   int wide_y, wide_z;           // every row starts on a 32-byte boundary
-  int mtiles, ntiles, group;    // tiles of 256 x 256; rows of tiles per group (see LinearWalk)
+  int mtiles, ntiles, group;    // tiles of 256 x kBN; rows of tiles per group (see LinearWalk)
   int* status;
 };
 
@@ -113,16 +113,18 @@ struct LinearWalk {
 };
 
 // kY32: y and residual are fp32.  kKeepZ: z is stored too.
-template <bool kY32, bool kKeepZ>
+template <bool kY32, bool kKeepZ, int kTileN>
 struct LinearEpi {
   using Params = LinearParams;
   using Walk = LinearWalk;
+  static constexpr int kBN = kTileN, kGroupN = PairCfg<kBN>::BNG;
+  static __device__ __forceinline__ int rows(const Params& p) { return p.M; }
   const Params& p;
-  int pair_row, quarter, lane, row;
+  int pair_row, group, lane, row;
   uint4 next[kY32 ? 8 : 4];  // residual of the next chunk: its loads run under the chunk before
   float bias[2];             // of this lane's column in either chunk
-  __device__ __forceinline__ LinearEpi(const Params& p_, int pair_row_, int quarter_)
-      : p(p_), pair_row(pair_row_), quarter(quarter_), lane(threadIdx.x & 31), row(0), bias{0.f, 0.f} {}
+  __device__ __forceinline__ LinearEpi(const Params& p_, int pair_row_, int group_)
+      : p(p_), pair_row(pair_row_), group(group_), lane(threadIdx.x & 31), row(0), bias{0.f, 0.f} {}
   __device__ __forceinline__ void fetch(int col0) {
     constexpr int kE = kY32 ? 4 : 2, kPerVec = 16 / kE, kVecs = 32 / kPerVec;
     if (p.residual == nullptr || row >= p.M) return;
@@ -146,11 +148,11 @@ struct LinearEpi {
   }
   __device__ __forceinline__ void begin(const PairTile& t) {
     row = t.row0 + pair_row;
-    const int col0 = t.tile * pair_cfg::BN + quarter * pair_cfg::BNQ;
+    const int col0 = t.tile * kBN + group * kGroupN;
     if (col0 < p.N) fetch(col0);
     if (p.bias != nullptr) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) bias[i] = col0 + 32 * i + lane < p.N ? linear_bias(p, col0 + 32 * i + lane) : 0.f;
+      for (int i = 0; i < kGroupN / 32; ++i) bias[i] = col0 + 32 * i + lane < p.N ? linear_bias(p, col0 + 32 * i + lane) : 0.f;
     }
   }
   __device__ __forceinline__ void chunk(const uint32_t (&acc)[32], int col0) {
@@ -161,7 +163,7 @@ struct LinearEpi {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(acc[i]);
     if (p.bias != nullptr) {
       // loaded once per warp, a column per lane, and handed round by shuffles
-      const float b = col0 % pair_cfg::BNQ == 0 ? bias[0] : bias[1];
+      const float b = col0 % kGroupN == 0 ? bias[0] : bias[1];
 #pragma unroll
       for (int i = 0; i < 32; ++i) v[i] += __shfl_sync(0xffffffffu, b, i);
     }
@@ -187,7 +189,7 @@ struct LinearEpi {
           }
         }
       }
-      const int last = (col0 / pair_cfg::BNQ + 1) * pair_cfg::BNQ;  // end of this quarter
+      const int last = (col0 / kGroupN + 1) * kGroupN;  // end of this group's columns
       if (col0 + 32 < min(last, p.N)) fetch(col0 + 32);
     }
     if (row < p.M)

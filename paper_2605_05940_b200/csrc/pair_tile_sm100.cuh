@@ -1,7 +1,7 @@
 // Tensor-core tiles of a product D[m,n] = sum_k A[m,k] B[n,k] with an epilogue of the user's choice:
 // the main loop behind the vocabulary cross entropy and the linear layer.
 //
-// Two CTAs on neighbouring SMs (a cluster of 2) work as a pair on a 256 x 256 tile with tcgen05
+// Two CTAs on neighbouring SMs (a cluster of 2) work as a pair on a 256 x 256 (or narrower) tile with tcgen05
 // .cta_group::2: each CTA stages its own 128 rows of A and its own 128 of the tile's 256 rows of B (both
 // K-major bf16, 128-byte swizzle), and its tensor memory receives its own 128 rows of the tile for all 256
 // columns.  Two accumulators (all 512 columns of tensor memory) let the epilogue of a tile run under the
@@ -14,8 +14,8 @@
 //               counted on the leader's "full" barrier
 //   warp 1      leader CTA (cluster rank 0) only: the MMA issuer of the pair.  In both CTAs this warp
 //               owns the tensor memory
-//   warps 2-17  epilogue: warp w reads tensor-memory lanes 32*(w%4).., columns 64*((w-2)/4).., so that
-//               every thread owns one row and a quarter of the tile's columns.  Sixteen warps, four per
+//   warps 2-17  epilogue: warp w reads tensor-memory lanes 32*(w%4).., columns of group (w-2)/4, so that
+//               every thread owns one row and a quarter (64 columns wide tiles: half) of the tile's columns.  Sixteen warps, four per
 //               scheduler: with eight (half a tile each) an epilogue with an activation was bound by its
 //               own latencies and took longer than the MMAs of a K = 1536 tile
 // An epilogue stores results the size of the tile from registers, 64 bytes of a row per thread and chunk
@@ -25,8 +25,10 @@
 //
 // Epi provides (Walk is evaluated by every role alike):
 //   Params                     launch parameters, with `int* status` and `int ksteps`
+//   rows(p)                    rows of A that exist
+//   kBN                        columns of a tile
 //   Walk(p, pair, pairs)       the tiles of a pair: bool next(PairTile&)
-//   Epi(p, row_local, quarter) per epilogue thread; then for every tile begin(tile), for every chunk of 32
+//   Epi(p, row_local, group)   per epilogue thread; then for every tile begin(tile), for every chunk of 32
 //                              columns chunk(acc[32], col0), and end(tile)
 #pragma once
 
@@ -36,7 +38,7 @@ namespace npd {
 
 struct PairTile {
   int row0;         // first row of the pair's 256; this CTA's rows start at row0 + 128 * rank
-  int tile;         // column tile (256 columns)
+  int tile;         // column tile (kBN columns)
   int run;          // epilogue's own number of the sequence of tiles this one belongs to
   bool first, last; // of that sequence
 };
@@ -70,28 +72,34 @@ __device__ __forceinline__ void store_row32(void* dst, const float (&v)[32], int
   }
 }
 
-namespace pair_cfg {
-constexpr int BM = 128, BN = 256, BK = 64, UK = 16;
-constexpr int BNH = BN / 2;
-constexpr int KS = 2, STAGES = 3;
-constexpr int A_BYTES = BM * BK * 2;
-constexpr int B_BYTES = BNH * BK * 2;
-constexpr int EPI_WARPS = 16;
-constexpr int BNQ = BN / 4;          // columns of an epilogue warp
-constexpr int THREADS = 64 + 32 * EPI_WARPS;
-constexpr int TMEM_COLS = 512;
-constexpr int OFF_A = 0;
-constexpr int OFF_B = OFF_A + STAGES * KS * A_BYTES;
-constexpr int OFF_BAR = OFF_B + STAGES * KS * B_BYTES;
-constexpr int NUM_BARS = 2 * STAGES + 4;
-constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
-}  // namespace pair_cfg
+// kBN = columns of a pair tile: 256, or 128 or 64 for problems that would not give every pair a tile otherwise.
+template <int kBN>
+struct PairCfg {
+  static constexpr int BM = 128, BN = kBN, BK = 64, UK = 16;
+  static constexpr int BNH = BN / 2;  // rows of B each CTA stages
+  static constexpr int KS = 2, STAGES = BN == 256 ? 3 : (BN == 128 ? 4 : 5);
+  static constexpr int A_BYTES = BM * BK * 2;
+  static constexpr int B_BYTES = BNH * BK * 2;
+  static constexpr int EPI_WARPS = 16;
+  static constexpr int GROUPS = BN >= 128 ? 4 : 2;  // groups of four epilogue warps that have columns
+  static constexpr int BNG = BN / GROUPS;           // columns of a group: 64 or 32
+  static constexpr int THREADS = 64 + 32 * EPI_WARPS;
+  static constexpr int TMEM_COLS = 2 * BN;
+  static constexpr int OFF_A = 0;
+  static constexpr int OFF_B = OFF_A + STAGES * KS * A_BYTES;
+  static constexpr int OFF_BAR = OFF_B + STAGES * KS * B_BYTES;
+  static constexpr int NUM_BARS = 2 * STAGES + 4;
+  static constexpr int SMEM_BYTES = OFF_BAR + NUM_BARS * 8 + 16 + 1024;
+};
 
 template <class Epi>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_cfg::THREADS, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<Epi::kBN>::THREADS, 1)
 pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                  const typename Epi::Params p) {
-  using namespace pair_cfg;
+  using L = PairCfg<Epi::kBN>;
+  constexpr int BM = L::BM, BN = L::BN, BK = L::BK, UK = L::UK, BNH = L::BNH, KS = L::KS, STAGES = L::STAGES, A_BYTES = L::A_BYTES,
+                B_BYTES = L::B_BYTES, GROUPS = L::GROUPS, BNG = L::BNG, OFF_A = L::OFF_A, OFF_B = L::OFF_B, OFF_BAR = L::OFF_BAR,
+                NUM_BARS = L::NUM_BARS, TMEM_COLS = L::TMEM_COLS;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
@@ -114,7 +122,7 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(tfull0 + 8 * b, 1);
-      mbar_init(tempty0 + 8 * b, 2 * EPI_WARPS);  // the epilogue warps of both CTAs, counted in the leader
+      mbar_init(tempty0 + 8 * b, 2 * 4 * GROUPS);  // the epilogue warps of both CTAs, counted in the leader
     }
     *abort_flag = 0;
     fence_mbar_init();
@@ -143,18 +151,22 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
+      const int rows = Epi::rows(p);
       while (ok && walk.next(t)) {
         const int ra = t.row0 + static_cast<int>(rank) * BM;
         const int rb = t.tile * BN + static_cast<int>(rank) * BNH;
+        // A CTA whose rows do not exist fetches none: what its rows of the tile hold is never stored.
+        const bool mine = ra < rows, both = t.row0 + BM < rows;
+        const uint32_t step_bytes = (both ? 2 : 1) * A_BYTES + 2 * B_BYTES;
         for (int ks = 0; ks < p.ksteps; ks += KS, ++it) {
           const uint32_t st = it % STAGES, ph = (it / STAGES) & 1;
           const int nk = min(KS, p.ksteps - ks);
           if (!(ok = mbar_wait(empty0 + 8 * st, ph ^ 1, abort_flag))) break;
           // the leader's barrier counts the bytes of both CTAs' loads of this stage
-          if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * st, 2 * nk * (A_BYTES + B_BYTES));
+          if (rank == 0) mbar_arrive_expect_tx(full0 + 8 * st, nk * step_bytes);
           const uint32_t fb = full_leader + 8 * st;
           for (int h = 0; h < nk; ++h) {
-            tma_load_2d_pair(smem_u32(smem + OFF_A + (st * KS + h) * A_BYTES), &tmap_a, fb, (ks + h) * BK, ra);
+            if (mine) tma_load_2d_pair(smem_u32(smem + OFF_A + (st * KS + h) * A_BYTES), &tmap_a, fb, (ks + h) * BK, ra);
             tma_load_2d_pair(smem_u32(smem + OFF_B + (st * KS + h) * B_BYTES), &tmap_b, fb, (ks + h) * BK, rb);
           }
         }
@@ -209,12 +221,11 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
         if (ok) umma_commit_pair(tfull0 + 8 * buf);
       }
     }
-  } else {
+  } else if (warp < 2 + 4 * GROUPS) {
     // ---------------------- epilogue ----------------------
-    const int e = warp - 2;
-    const int lg = warp & 3;     // the lane group of tensor memory this warp may read
-    const int quarter = e >> 2;  // which 64 columns of the tile
-    Epi epi(p, static_cast<int>(rank) * BM + lg * 32 + lane, quarter);
+    const int lg = warp & 3;            // the lane group of tensor memory this warp may read
+    const int group = (warp - 2) >> 2;  // which BNG columns of the tile
+    Epi epi(p, static_cast<int>(rank) * BM + lg * 32 + lane, group);
     uint32_t tile = 0;
     bool ok = true;
     for (; ok && walk.next(t); ++tile) {
@@ -222,20 +233,20 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
       epi.begin(t);
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(tfull0 + 8 * buf, tph, abort_flag)))) break;
       tc_fence_after_sync();
-      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(lg * 32) << 16) + buf * BN + quarter * BNQ;
+      const uint32_t taddr = tmem_base + (static_cast<uint32_t>(lg * 32) << 16) + buf * BN + group * BNG;
 #pragma unroll 1
-      for (int c = 0; c < BNQ / 32; ++c) {
+      for (int c = 0; c < BNG / 32; ++c) {
         uint32_t acc[32];
         __syncwarp();  // the epilogue's branches may have parted the warp
         tmem_ld32(taddr + c * 32, acc);
         tmem_ld_wait();
-        if (c == BNQ / 32 - 1) {
+        if (c == BNG / 32 - 1) {
           // everything this warp needs of the accumulator is in registers: it may be overwritten
           tc_fence_before_sync();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(tempty_leader + 8 * buf);
         }
-        epi.chunk(acc, t.tile * BN + quarter * BNQ + c * 32);
+        epi.chunk(acc, t.tile * BN + group * BNG + c * 32);
       }
       epi.end(t);
     }
