@@ -31,6 +31,7 @@
  *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless the comment says HOST.
+ *   - The device that holds the buffers, and that the stream belongs to, has to be the current one.
  *   - The caller owns every buffer.  The library allocates no device memory,
  *     keeps no problem state between calls and only enqueues work on the given stream
  *     (a cudaStream_t passed as void*; NULL = the legacy default stream).
@@ -63,7 +64,8 @@ extern "C" {
 typedef enum npd_status {
   NPD_OK = 0,
   NPD_EINVAL = -1,      /* null pointer, bad size field, non-positive dimension, tau <= 0 */
-  NPD_ESHAPE = -2,      /* d not a multiple of 64, a row stride smaller than the row, S > T */
+  NPD_ESHAPE = -2,      /* d not a multiple of 64, a row stride smaller than the row, S > T, an extent beyond the
+                           documented limits */
   NPD_EALIGN = -3,      /* a base pointer or row stride of a tensor operand not 16-byte aligned */
   NPD_ESEQ = -4,        /* cu_seqlens malformed (found on the device) */
   NPD_EARCH = -5,       /* current device is not compute capability 10.x */
@@ -431,7 +433,7 @@ enum {
  * Either gradient may be NULL (a frozen head, for instance); the work for it is then left out.
  *
  * Layouts and alignment as in npd_kd_args: row-major, row strides in ELEMENTS, the four matrices 16-byte
- * aligned with row strides that are multiples of 16 bytes, d a multiple of 64, any T >= 1, V >= 1.  Outputs may not
+ * aligned with row strides that are multiples of 16 bytes, d a multiple of 64, any T >= 1, V >= 1 with T V <= 2^46.  Outputs may not
  * overlap inputs or each other (NPD_EINVAL).
  *
  * nll, lse and d_weight are bitwise reproducible; d_hidden is summed over pieces of the vocabulary with
@@ -496,7 +498,7 @@ enum { NPD_LINEAR_ACCUMULATE_DW = 1 /* add into dw instead of overwriting it (f3
  * and dw (dbias sums the unrounded values), so an fp32 dw has fp32 sums of bf16-rounded terms.
  *
  * Row-major, row strides in ELEMENTS, matrices on 16-byte boundaries with row strides that are multiples of 16
- * bytes; any M, N, K >= 1.  bias needs no alignment beyond its type's.  y may be residual itself (same pointer and
+ * bytes; any M, N, K >= 1 with M N, M K and N K <= 2^46.  bias needs no alignment beyond its type's.  y may be residual itself (same pointer and
  * stride); any other overlap of a result with an operand or another result is refused (NPD_EINVAL).
  *
  * Every result is bitwise reproducible, but for a dw that is added to (atomic adds, one per element and call).
@@ -551,7 +553,7 @@ enum { NPD_NORM_POST = 1 /* the branch goes through a norm of its own before it 
  * gains are of `weight_dtype`, their gradients fp32.  All arithmetic is fp32 and each result is rounded once;
  * y is taken from the unrounded h.  Layouts are row-major with row strides in ELEMENTS; every matrix
  * starts on a 16-byte boundary with a row stride that is a multiple of 16 bytes, the gains need no
- * alignment beyond their type's.  Any T >= 1 and 1 <= d <= 16384 (d need not be a multiple of anything).
+ * alignment beyond their type's.  Any 1 <= T <= 2^30 and 1 <= d <= 16384 (d need not be a multiple of anything).
  * gate has a row per token, or with ldg = 0 one row that all tokens share.
  *
  * In place: h may be residual or x, y may be x or residual (same pointer, type and stride); dx, dresidual

@@ -66,6 +66,7 @@ int check_ce(const npd_ce_args* a, bool need_pointers) {
   if ((a->flags & NPD_CE_ACCUMULATE_DW) && a->d_weight_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
   // row numbers and 256-wide tiles are 32-bit
   if (a->T > (1 << 30) || a->V > (1 << 30)) return NPD_ESHAPE;
+  if ((a->T / 256 + 1ll) * (a->V / 256 + 1ll) > (1 << 30)) return NPD_ESHAPE;
   if (a->d % 64 != 0) return NPD_ESHAPE;
   if (!need_pointers) return NPD_OK;
   if (a->hidden == nullptr || a->weight == nullptr || a->labels == nullptr || a->nll == nullptr) return NPD_EINVAL;

@@ -185,7 +185,7 @@ struct CeWalk {
     u = pair - num_pairs;
     step = num_pairs;
     vt = vt1 = row0 = run = 0;
-    group = p.group_pairs;
+    group = max(1, min(p.group_pairs, pairs));
     vt_begin = p.vt_begin;
     vt_count = p.vt_count;
     fresh = false;

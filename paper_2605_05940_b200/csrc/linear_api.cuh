@@ -168,7 +168,7 @@ int npd_linear_fwd(const npd_linear_args* a, void* cuda_stream) {
     return e == cudaSuccess ? NPD_OK : NPD_ECUDA;
   }
   p.mtiles = (a->M + 255) / 256;
-  p.group = static_cast<int>(std::max<long long>(4, (32ll << 20) / (512ll * a->K)));
+  p.group = static_cast<int>(std::min<long long>(p.mtiles, std::max<long long>(4, (32ll << 20) / (512ll * a->K))));
   if (p.y_f32)
     return p.z != nullptr ? launch_linear_tiles<true, true>(a, p, di.sms, st) : launch_linear_tiles<true, false>(a, p, di.sms, st);
   return p.z != nullptr ? launch_linear_tiles<false, true>(a, p, di.sms, st) : launch_linear_tiles<false, false>(a, p, di.sms, st);

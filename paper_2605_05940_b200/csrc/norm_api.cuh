@@ -40,10 +40,10 @@ struct NormPlan {
 NormPlan norm_plan(const npd_norm_args* a, int sms, bool backward) {
   using namespace norm_cfg;
   NormPlan pl{};
-  pl.vec = a->d <= kMaxSmallD ? 1 : (a->d <= 2 * kMaxSmallD ? 2 : 4);
+  pl.vec = a->d <= (backward ? kMaxSmallBwd : kMaxSmallFwd) ? 1 : (a->d <= kMaxSmallFwd ? 2 : 4);
   const int per = 8 * pl.vec;
   pl.threads = ((a->d + per - 1) / per + 31) / 32 * 32;
-  pl.smem = backward && pl.vec > 1 ? 2 * a->d * static_cast<int>(sizeof(float)) : 0;  // sums over rows
+  pl.smem = backward && pl.vec > 1 ? 64 * pl.vec * pl.threads : 0;  // sums over rows
   // Resident CTAs per SM, by threads and (an estimate of) registers: every CTA goes through its share
   // of the rows.  Several per SM, so that one CTA's barriers run under another one's loads.
   int per_sm = (pl.vec > 1 ? 512 : (!backward ? 1024 : (pl.threads <= 256 ? 816 : 512))) / pl.threads;
@@ -57,7 +57,7 @@ NormPlan norm_plan(const npd_norm_args* a, int sms, bool backward) {
 int check_norm(const npd_norm_args* a, bool backward, bool need_pointers) {
   if (a == nullptr || a->size != sizeof(npd_norm_args)) return NPD_EINVAL;
   if (a->T < 1 || a->d < 1) return NPD_EINVAL;
-  if (a->d > norm_cfg::kMaxD) return NPD_ESHAPE;
+  if (a->d > norm_cfg::kMaxD || a->T > (1 << 30)) return NPD_ESHAPE;
   if (a->stream_dtype != NPD_DTYPE_BF16 && a->stream_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
   if (a->weight_dtype != NPD_DTYPE_BF16 && a->weight_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
   if (a->flags & ~NPD_NORM_POST) return NPD_EINVAL;
@@ -176,11 +176,12 @@ NormParams norm_params(const npd_norm_args* a, bool backward) {
 }
 
 template <bool kF32>
-void (*norm_bwd_pick(const NormPlan& pl, bool full))(NormParams) {
-  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, false, 512, 1>;
-  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, false, 512, 1>;
-  if (pl.threads <= 256) return full ? norm_bwd_kernel<kF32, 1, true, 256, 3> : norm_bwd_kernel<kF32, 1, false, 256, 2>;
-  return full ? norm_bwd_kernel<kF32, 1, true, 512, 1> : norm_bwd_kernel<kF32, 1, false, 512, 1>;
+void (*norm_bwd_pick(const NormPlan& pl, int form))(NormParams) {
+  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, 0, 512, 1>;
+  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, 0, 512, 1>;
+  if (pl.threads <= 256)
+    return form == 2 ? norm_bwd_kernel<kF32, 1, 2, 256, 3> : form == 1 ? norm_bwd_kernel<kF32, 1, 1, 256, 3> : norm_bwd_kernel<kF32, 1, 0, 256, 2>;
+  return form == 2 ? norm_bwd_kernel<kF32, 1, 2, 512, 1> : form == 1 ? norm_bwd_kernel<kF32, 1, 1, 512, 1> : norm_bwd_kernel<kF32, 1, 0, 512, 1>;
 }
 
 }  // namespace
@@ -206,9 +207,8 @@ int npd_norm_fwd(const npd_norm_args* a, void* cuda_stream) {
   if (di.cc_major != 10) return NPD_EARCH;
   const NormPlan pl = norm_plan(a, di.sms, false);
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
-  auto k = pl.vec == 1   ? (sf ? norm_fwd_kernel<true, 1> : norm_fwd_kernel<false, 1>)
-           : pl.vec == 2 ? (sf ? norm_fwd_kernel<true, 2> : norm_fwd_kernel<false, 2>)
-                         : (sf ? norm_fwd_kernel<true, 4> : norm_fwd_kernel<false, 4>);
+  auto k = pl.vec == 1 ? (sf ? norm_fwd_kernel<true, 1> : norm_fwd_kernel<false, 1>)
+                       : (sf ? norm_fwd_kernel<true, 4> : norm_fwd_kernel<false, 4>);
   const cudaError_t e = launch_ex(k, pl.grid, pl.threads, 0, static_cast<cudaStream_t>(cuda_stream), false,
                                   norm_params(a, false));
   ++g_launches;
@@ -232,9 +232,10 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   }
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool full = pl.vec == 1 && a->d % 256 == 0 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr &&
+  const bool full = pl.vec == 1 && a->d % 8 == 0 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr &&
                     p.dres != nullptr && (p.gate == nullptr || p.ldg == 0);
-  auto k = sf ? norm_bwd_pick<true>(pl, full) : norm_bwd_pick<false>(pl, full);
+  const int form = !full ? 0 : (a->d % 256 == 0 ? 2 : 1);
+  auto k = sf ? norm_bwd_pick<true>(pl, form) : norm_bwd_pick<false>(pl, form);
   // without the full form's registers fewer CTAs are resident (the workspace is sized for the larger number)
   const int grid = full ? pl.grid : std::min(pl.grid, di.sms * std::max(1, 512 / pl.threads));
   const int smem = full && !sf ? norm_cfg::kRing * pl.threads * 16 * 4 : pl.smem;

@@ -54,11 +54,10 @@ struct NormParams {
 
 namespace norm_cfg {
 constexpr int kMaxD = 16384;
-// A row takes at most 512 threads (128 registers each).  Up to d = 4096 that is one vector of eight
-// per thread, with gains, sums over rows and the next row's loads in registers; beyond, two or four
-// vectors per thread, gains re-read (they sit in L1/L2), the sums in shared memory and no prefetch: the
-// data of two vectors alone fill the registers, and a row is then long enough to cover its latency.
-constexpr int kMaxSmallD = 4096;
+// One vector of eight per thread, gains (and sums over rows) in registers, up to d = 8192 (1024 threads of 64
+// registers) in the forward and 4096 (512 threads of 128) in the backward; beyond, two or four vectors per thread
+// (at most 512 of them), gains re-read (they sit in L1/L2), sums over rows in shared memory.
+constexpr int kMaxSmallFwd = 8192, kMaxSmallBwd = 4096;
 constexpr int kMaxThreads = 512;
 constexpr int kMaxSmem = 2 * kMaxD * 4;  // dynamic shared memory a launch may ask for: sums over the widest row
 constexpr int kRing = 2;  // rows in flight per CTA of the backward
@@ -157,6 +156,12 @@ __device__ __forceinline__ V8 gain8(const void* w, int w_f32, float offset, int 
     return o;
   }
   // the gains need not be 16-byte aligned: a parameter may be a slice of a larger one
+  if ((reinterpret_cast<uintptr_t>(w) & 15u) == 0 && c + 8 <= d) {
+    o = w_f32 ? unpack8<true>(load8<true>(w, c, d)) : unpack8<false>(load8<false>(w, c, d));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] += offset;
+    return o;
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     float v = 0.f;
@@ -237,17 +242,18 @@ __device__ __forceinline__ uint4 ring_get(uint32_t addr) {
 
 // Sums of N values over the block, the same in every thread, in a fixed order.  One barrier; the caller
 // alternates `buf` so that a second call may write while slow threads still read the first one's numbers.
-// At most 16 warps; the places of warps that do not exist hold zeros.
+// The places of warps that do not exist hold zeros.
 template <int N>
 struct SumBuf {
-  float4 v[N][4];
+  float4 v[N][8];
 };
 template <int N>
 __device__ __forceinline__ void clear_sums(SumBuf<N>* buf, int count) {
   float* f = reinterpret_cast<float*>(buf);
-  for (int i = threadIdx.x; i < count * N * 16; i += blockDim.x) f[i] = 0.f;
+  for (int i = threadIdx.x; i < count * N * 32; i += blockDim.x) f[i] = 0.f;
 }
-template <int N>
+// kWide: the block may have more than 16 warps.
+template <int N, bool kWide = false>
 __device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
@@ -266,6 +272,10 @@ __device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
       const float4 c = buf.v[k][2], e = buf.v[k][3];
       s[k] += ((c.x + c.y) + (c.z + c.w)) + ((e.x + e.y) + (e.z + e.w));
     }
+    if (kWide && warps > 16) {
+      const float4 c = buf.v[k][4], e = buf.v[k][5], f = buf.v[k][6], g = buf.v[k][7];
+      s[k] += (((c.x + c.y) + (c.z + c.w)) + ((e.x + e.y) + (e.z + e.w))) + (((f.x + f.y) + (f.z + f.w)) + ((g.x + g.y) + (g.z + g.w)));
+    }
   }
 }
 
@@ -274,7 +284,7 @@ __device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
 
 // Forward.  kVec vectors of eight per thread; vector j of a thread starts at 8 * (threadIdx + j * blockDim).
 template <bool kF32, int kVec>
-__global__ void __launch_bounds__(norm_cfg::kMaxThreads, kVec == 1 ? 2 : 1) norm_fwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kVec == 1 ? 1024 : norm_cfg::kMaxThreads) norm_fwd_kernel(const NormParams p) {
   __shared__ SumBuf<1> red[4];
   constexpr bool kHold = kVec == 1;  // gains held in registers, the next row's loads in flight
   constexpr size_t es = kF32 ? 4 : 2;
@@ -331,7 +341,7 @@ __global__ void __launch_bounds__(norm_cfg::kMaxThreads, kVec == 1 ? 2 : 1) norm
         for (int i = 0; i < 4; ++i) q = fma2(x.p[i], x.p[i], q);
       }
       float s[1] = {sum2(q)};
-      block_sum<1>(s, red[2 * par]);
+      block_sum<1, kVec == 1>(s, red[2 * par]);
       scale *= rsqrtf(fmaf(s[0], inv_d, p.eps));
     }
     const unsigned long long scale2 = pair2(scale, scale), res2 = pair2(p.res_scale, p.res_scale);
@@ -358,7 +368,7 @@ __global__ void __launch_bounds__(norm_cfg::kMaxThreads, kVec == 1 ? 2 : 1) norm
     }
     if (p.y == nullptr) continue;
     float s[1] = {sum2(q)};
-    block_sum<1>(s, red[2 * par + 1]);
+    block_sum<1, kVec == 1>(s, red[2 * par + 1]);
     const float rh = rsqrtf(fmaf(s[0], inv_d, p.eps));
     const unsigned long long rh2 = pair2(rh, rh);
 #pragma unroll
@@ -379,17 +389,18 @@ __global__ void __launch_bounds__(norm_cfg::kMaxThreads, kVec == 1 ? 2 : 1) norm
 // and loads; with prefetched rows as well, three warps per scheduler waited for their own shuffles, and with
 // gains in shared memory that memory's pipe was the limit).  Otherwise the sums are in shared memory
 // (dynamic, [2][d]) and gains are re-read.
-// kFull: every operand and result exists, no per-token gate, d a multiple of 256 (no thread or vector is
-// partly outside the row): the same arithmetic without the tests for it.  With a bf16 stream rows then arrive
+// kForm > 0: every operand and result exists, no per-token gate, d a multiple of 8 (no vector is partly outside the
+// row); 2: of 256 (no thread is outside it): the same arithmetic without the tests for it (d = 1536 with form 1:
+// 230 us instead of 198 at T = 65,536; d = 1000 with form 0: 78 us instead of 50 at T = 16,384).  With a bf16 stream rows then arrive
 // through a ring of kRing stages in shared memory (asynchronous copies, two rows ahead), so that loads are in
 // flight during the reductions without taking registers: T = 65,536, d = 1536 takes 198 us with it and 259 us
 // without.  With an fp32 stream the ring is slower (387 us against 315 us).
-template <bool kF32, int kVec, bool kFull, int kThreads, int kBlocks>
+template <bool kF32, int kVec, int kForm, int kThreads, int kBlocks>
 __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormParams p) {
   __shared__ SumBuf<3> red3[2];
   __shared__ SumBuf<1> red1[2];
   extern __shared__ __align__(16) float dyn[];  // sums over rows, or the ring
-  constexpr bool kHold = kVec == 1;
+  constexpr bool kHold = kVec == 1, kFull = kForm > 0;
   constexpr int kRing = norm_cfg::kRing;
   constexpr bool kRows = kFull && !kF32;  // rows arrive through the ring
   constexpr size_t es = kF32 ? 4 : 2;
@@ -411,6 +422,8 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     for (int i = 0; i < 8; ++i) w.v[i] *= p.branch_scale * g.v[i];
     return pack8(w);
   };
+  // !kHold: the sums, [sum][vector][half] planes of 16 bytes per thread
+  ulonglong2* sums = reinterpret_cast<ulonglong2*>(dyn);
   auto gain = [&](int which, int j) {
     return kHold ? held[which] : read_gain(which, 8 * (static_cast<int>(threadIdx.x) + j * nt));
   };
@@ -422,22 +435,22 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     held[1] = read_gain(1, 8 * static_cast<int>(threadIdx.x));
   } else {
     // every thread clears, adds to and reads back its own columns only: no barrier needed
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        for (int i = 0; i < 8; ++i) {
-          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
-          if (c < p.d) dyn[a * p.d + c] = 0.f;
-        }
+    for (int i = 0; i < 4 * kVec; ++i) sums[i * nt + threadIdx.x] = make_ulonglong2(0ull, 0ull);
   }
   __syncthreads();
   struct Row {
     Raw8<false> dy[kVec], x[kVec], g[kVec];
     Raw8<kF32> h[kVec], dh[kVec];
   };
-  const int d_ = kFull ? 1 << 30 : p.d;  // kFull: no vector reaches past the row
+  const int d_ = kFull ? 1 << 30 : p.d;  // kFull: no vector reaches past the row ...
+  const bool active = kForm != 1 || 8 * static_cast<int>(threadIdx.x) < p.d;  // ... and threads beyond it hold zeros
   auto fetch = [&](int t) {
     Row o;
+    if (!active) {
+      o.dy[0] = o.x[0] = zero8<false>();
+      o.h[0] = o.dh[0] = zero8<kF32>();
+      return o;
+    }
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
       const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
@@ -458,7 +471,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
   constexpr int kSlots = 4;
   const uint32_t slot = 16u * static_cast<uint32_t>(nt), ring0 = smem_u32(dyn) + 16u * threadIdx.x;
   auto issue = [&](int t, int stage) {
-    if (t < p.T) {
+    if (t < p.T && active) {
       const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
       async_copy16(at, p.dy + static_cast<size_t>(t) * p.lddy + 8 * threadIdx.x);
       async_copy16(at + slot, p.x + static_cast<size_t>(t) * p.ldx + 8 * threadIdx.x);
@@ -469,6 +482,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
   };
   auto take = [&](int stage) {
     Row o;
+    if (!active) {
+      o.dy[0].q[0] = o.x[0].q[0] = o.h[0].q[0] = o.dh[0].q[0] = make_uint4(0u, 0u, 0u, 0u);
+      return o;
+    }
     const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
     o.dy[0].q[0] = ring_get(at);
     o.x[0].q[0] = ring_get(at + slot);
@@ -518,7 +535,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
       const P8 dy = pairs8<false>(cur.dy[j]), h = pairs8<kF32>(cur.h[j]), x = pairs8<false>(cur.x[j]),
                dh = pairs8<kF32>(cur.dh[j]);
       const P8 wq = gain(0, j), G = gain(1, j);
-      P8 o, dg, g;
+      P8 o, dg, g, a0, a1, d2s;
       if (token_gate) g = pairs8<false>(cur.g[j]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -537,19 +554,22 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
           acc[0].p[i] = fma2(mul2(dy.p[i], h.p[i]), rh2, acc[0].p[i]);
           acc[1].p[i] = fma2(d2, xn, acc[1].p[i]);
         } else {
-          const float2 b0 = unpair2(mul2(mul2(dy.p[i], h.p[i]), rh2)), b1 = unpair2(mul2(d2, xn));
-          const int e = c + 2 * i;
-          if (e < p.d) {
-            dyn[e] += b0.x;
-            dyn[p.d + e] += b1.x;
-          }
-          if (e + 1 < p.d) {
-            dyn[e + 1] += b0.y;
-            dyn[p.d + e + 1] += b1.y;
-          }
+          a0.p[i] = mul2(dy.p[i], h.p[i]);
+          a1.p[i] = xn;
+          d2s.p[i] = d2;
         }
       }
-      if (kFull || p.dres != nullptr)
+      if (!kHold) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          ulonglong2* u = sums + (2 * j + half) * nt + threadIdx.x;
+          ulonglong2* w = sums + (2 * (kVec + j) + half) * nt + threadIdx.x;
+          const ulonglong2 su = *u, sw = *w;
+          *u = make_ulonglong2(fma2(a0.p[2 * half], rh2, su.x), fma2(a0.p[2 * half + 1], rh2, su.y));
+          *w = make_ulonglong2(fma2(d2s.p[2 * half], a1.p[2 * half], sw.x), fma2(d2s.p[2 * half + 1], a1.p[2 * half + 1], sw.y));
+        }
+      }
+      if (kFull ? active : p.dres != nullptr)
         store8<kF32>(static_cast<char*>(p.dres) + static_cast<size_t>(t) * p.lddres * es, c, d_, o);
       if (token_gate && p.dgate != nullptr) store8<false>(p.dgate + static_cast<size_t>(t) * p.lddgate, c, d_, dg);
     }
@@ -566,6 +586,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
         for (int i = 0; i < 4; ++i) vv[j].p[i] = mul2(rx2, fma2(x.p[i], cx2, vv[j].p[i]));
       }
     }
+    if (!active) continue;
 #pragma unroll
     for (int j = 0; j < kVec; ++j)
       store8<false>(p.dx + static_cast<size_t>(t) * p.lddx, 8 * (static_cast<int>(threadIdx.x) + j * nt), d_, vv[j]);
@@ -586,9 +607,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
-        for (int i = 0; i < 8; ++i) {
-          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + i;
-          if (c < p.part_d) part[static_cast<size_t>(a) * p.part_d + c] = c < p.d ? dyn[a * p.d + c] : 0.f;
+        for (int half = 0; half < 2; ++half) {
+          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + 4 * half;
+          if (c < p.part_d)
+            *reinterpret_cast<ulonglong2*>(part + static_cast<size_t>(a) * p.part_d + c) = sums[(2 * (a * kVec + j) + half) * nt + threadIdx.x];
         }
   }
 }

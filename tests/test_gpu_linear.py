@@ -188,6 +188,25 @@ def test_same_bits_other_stream_and_graph():
         assert torch.equal(y, y3) and all(torch.equal(p, q) for p, q in zip(want, got))
 
 
+def test_offsets_pass_32_bits():
+    # more than 2^31 results: the last rows and columns against fp64
+    g = torch.Generator(device=DEV).manual_seed(13)
+    M, N, K = 40011, 60008, 64
+    x, w = _mat(g, M, K), _mat(g, N, K, std=0.1)
+    y, z = B.npd_linear_fwd(x, w, activation=B.NPD_ACT_SILU, want_preact=True)
+    for rows, cols in ((slice(M - 40, M), slice(N - 300, N)), (slice(35000, 35040), slice(0, 300))):
+        _check_forward(x[rows], w[cols], None, None, "silu", y[rows, cols], z[rows, cols])
+    dy = y                                    # any values: its gradient of the inputs at sampled places
+    dx, _, db = B.npd_linear_bwd(dy, None, w, preact=z, activation=B.NPD_ACT_SILU, want_dw=False, want_dbias=True)
+    D, Z = dy[M - 20:].double(), z[M - 20:].double()
+    s = torch.sigmoid(Z)
+    dz = D * s * (1 + Z * (1 - s))
+    ref, big = dz @ w.double(), dz.abs() @ w.double().abs()
+    # the rounding of dz, the accumulation over N, the result's rounding
+    bound = u(BF16) * 1.01 * ref.abs() + (u(BF16) * 1.01 + 2 * u(F32) * (N / 16 + 64)) * big
+    assert bool(((dx[M - 20:].double() - ref).abs() <= bound).all())
+
+
 def test_a_large_case_against_fp64_on_the_gpu():
     g = torch.Generator(device=DEV).manual_seed(12)
     x, w, r = _mat(g, 4100, 1000), _mat(g, 2300, 1000, std=0.03), _mat(g, 4100, 2300)
@@ -200,3 +219,17 @@ def test_a_large_case_against_fp64_on_the_gpu():
     dx, dw, _ = B.npd_linear_bwd(dy, x, w)
     rel = lambda a, ref: float((a.double() - ref).norm() / ref.norm())
     assert rel(dx, dy.double() @ w.double()) < u(BF16) and rel(dw, dy.double().t() @ x.double()) < u(BF16)
+
+
+def test_plain_product_leaves_what_lies_beyond_its_last_column():
+    g = torch.Generator(device=DEV).manual_seed(14)
+    for M, N, K in ((70, 5, 40), (300, 515, 72), (33, 1, 8)):
+        a, b = _mat(g, M, K), _mat(g, N, K)
+        ref = host(a) @ host(b).T
+        for mode, dt in ((B.NPD_GEMM_STORE_F32, F32), (B.NPD_GEMM_ADD_F32, F32), (B.NPD_GEMM_STORE_BF16, BF16)):
+            buf = _out(M, N, dt)
+            buf[:, :N] = 0
+            B.npd_gemm_bf16(a, b, buf[:, :N], out_mode=mode)
+            assert torch.isnan(buf[:, N:]).all()
+            bound = u(dt) * np.abs(ref) * 1.01 + 2 * u(F32) * (K / 16 + 16) * (np.abs(host(a)) @ np.abs(host(b)).T)
+            assert np.all(np.abs(host(buf[:, :N]) - ref) <= bound)
