@@ -333,11 +333,18 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const LinearGradParams p
 #pragma unroll
   for (int i = 0; i < 8; ++i) s.v[i] = 0.f;
   if (c < p.N) {
-#pragma unroll 2
+    // the next row's loads are in flight while this row's slopes are evaluated
+    Raw8<false> dy = zero8<false>(), zz = zero8<false>();
+    auto fetch = [&](int m) {
+      dy = load8<false>(p.dy + static_cast<size_t>(m) * p.lddy, c, p.N);
+      if (kAct != kActNone) zz = load8<false>(p.z + static_cast<size_t>(m) * p.ldz, c, p.N);
+    };
+    if (m0 + warp < m1) fetch(m0 + warp);
     for (int m = m0 + warp; m < m1; m += 8) {
-      V8 g = unpack8<false>(load8<false>(p.dy + static_cast<size_t>(m) * p.lddy, c, p.N));
+      V8 g = unpack8<false>(dy);
+      const V8 z = unpack8<false>(zz);
+      if (m + 8 < m1) fetch(m + 8);
       if (kAct != kActNone) {
-        const V8 z = unpack8<false>(load8<false>(p.z + static_cast<size_t>(m) * p.ldz, c, p.N));
 #pragma unroll
         for (int i = 0; i < 8; ++i) g.v[i] *= act_slope(kAct, z.v[i]);
         store8<false>(p.dz + static_cast<size_t>(m) * p.lddz, c, p.N, g);
