@@ -207,8 +207,9 @@ int npd_norm_fwd(const npd_norm_args* a, void* cuda_stream) {
   if (di.cc_major != 10) return NPD_EARCH;
   const NormPlan pl = norm_plan(a, di.sms, false);
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
-  auto k = pl.vec == 1 ? (sf ? norm_fwd_kernel<true, 1> : norm_fwd_kernel<false, 1>)
-                       : (sf ? norm_fwd_kernel<true, 4> : norm_fwd_kernel<false, 4>);
+  auto k = pl.vec > 1          ? (sf ? norm_fwd_kernel<true, 4, 512> : norm_fwd_kernel<false, 4, 512>)
+           : pl.threads <= 512 ? (sf ? norm_fwd_kernel<true, 1, 512> : norm_fwd_kernel<false, 1, 512>)
+                               : (sf ? norm_fwd_kernel<true, 1, 1024> : norm_fwd_kernel<false, 1, 1024>);
   const cudaError_t e = launch_ex(k, pl.grid, pl.threads, 0, static_cast<cudaStream_t>(cuda_stream), false,
                                   norm_params(a, false));
   ++g_launches;

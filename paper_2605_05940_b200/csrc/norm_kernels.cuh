@@ -147,7 +147,9 @@ __device__ __forceinline__ void store8(void* row, int c, int d, const V8& a) {
     }
   }
 }
-// Gains w[c..c+8) + offset (0 beyond d; 1 without a gain).
+// Gains w[c..c+8) + offset (0 beyond d; 1 without a gain).  kWide: with 16-byte loads where the address allows it,
+// for the kernels that read their gains again for every row.
+template <bool kWide>
 __device__ __forceinline__ V8 gain8(const void* w, int w_f32, float offset, int c, int d) {
   V8 o;
   if (w == nullptr) {
@@ -156,7 +158,7 @@ __device__ __forceinline__ V8 gain8(const void* w, int w_f32, float offset, int 
     return o;
   }
   // the gains need not be 16-byte aligned: a parameter may be a slice of a larger one
-  if ((reinterpret_cast<uintptr_t>(w) & 15u) == 0 && c + 8 <= d) {
+  if (kWide && (reinterpret_cast<uintptr_t>(w) & 15u) == 0 && c + 8 <= d) {
     o = w_f32 ? unpack8<true>(load8<true>(w, c, d)) : unpack8<false>(load8<false>(w, c, d));
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.v[i] += offset;
@@ -283,8 +285,8 @@ __device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
 // missing operand zeros, and a branch without a norm has r_x = 1.
 
 // Forward.  kVec vectors of eight per thread; vector j of a thread starts at 8 * (threadIdx + j * blockDim).
-template <bool kF32, int kVec>
-__global__ void __launch_bounds__(kVec == 1 ? 1024 : norm_cfg::kMaxThreads) norm_fwd_kernel(const NormParams p) {
+template <bool kF32, int kVec, int kThreads>
+__global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) norm_fwd_kernel(const NormParams p) {
   __shared__ SumBuf<1> red[4];
   constexpr bool kHold = kVec == 1;  // gains held in registers, the next row's loads in flight
   constexpr size_t es = kF32 ? 4 : 2;
@@ -296,14 +298,14 @@ __global__ void __launch_bounds__(kVec == 1 ? 1024 : norm_cfg::kMaxThreads) norm
   grid_launch_dependents();
   auto gains = [&](int j) {
     const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-    V8 w = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
+    V8 w = gain8<!kHold>(p.w_post, p.w_f32, p.offset, c, p.d);
     if (p.gate != nullptr && !token_gate) {
       const V8 g = unpack8<false>(load8<false>(p.gate, c, p.d));
 #pragma unroll
       for (int i = 0; i < 8; ++i) w.v[i] *= g.v[i];
     }
     wp[j] = pack8(w);
-    wq[j] = pack8(gain8(p.w_pre, p.w_f32, p.offset, c, p.d));
+    wq[j] = pack8(gain8<!kHold>(p.w_pre, p.w_f32, p.offset, c, p.d));
   };
   if (kHold) gains(0);
   clear_sums(red, 4);
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(kVec == 1 ? 1024 : norm_cfg::kMaxThreads) norm
         for (int i = 0; i < 4; ++i) q = fma2(x.p[i], x.p[i], q);
       }
       float s[1] = {sum2(q)};
-      block_sum<1, kVec == 1>(s, red[2 * par]);
+      block_sum<1, (kThreads > 512)>(s, red[2 * par]);
       scale *= rsqrtf(fmaf(s[0], inv_d, p.eps));
     }
     const unsigned long long scale2 = pair2(scale, scale), res2 = pair2(p.res_scale, p.res_scale);
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(kVec == 1 ? 1024 : norm_cfg::kMaxThreads) norm
     }
     if (p.y == nullptr) continue;
     float s[1] = {sum2(q)};
-    block_sum<1, kVec == 1>(s, red[2 * par + 1]);
+    block_sum<1, (kThreads > 512)>(s, red[2 * par + 1]);
     const float rh = rsqrtf(fmaf(s[0], inv_d, p.eps));
     const unsigned long long rh2 = pair2(rh, rh);
 #pragma unroll
@@ -412,11 +414,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
   P8 held[2];  // kHold: gain of y, G
 #pragma unroll
   for (int i = 0; i < 4; ++i) acc[0].p[i] = acc[1].p[i] = held[0].p[i] = held[1].p[i] = 0ull;
-  auto shared_gate8 = [&](int c) { return shared_gate ? unpack8<false>(load8<false>(p.gate, c, p.d)) : gain8(nullptr, 0, 0.f, c, p.d); };
+  auto shared_gate8 = [&](int c) { return shared_gate ? unpack8<false>(load8<false>(p.gate, c, p.d)) : gain8<!kHold>(nullptr, 0, 0.f, c, p.d); };
   // which: 0 = gain of y, 1 = G (without a per-token gate)
   auto read_gain = [&](int which, int c) {
-    if (which == 0) return pack8(gain8(p.w_pre, p.w_f32, p.offset, c, p.d));
-    V8 w = gain8(p.w_post, p.w_f32, p.offset, c, p.d);
+    if (which == 0) return pack8(gain8<!kHold>(p.w_pre, p.w_f32, p.offset, c, p.d));
+    V8 w = gain8<!kHold>(p.w_post, p.w_f32, p.offset, c, p.d);
     const V8 g = shared_gate8(c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) w.v[i] *= p.branch_scale * g.v[i];
