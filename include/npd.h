@@ -29,6 +29,10 @@
  * ablation (flags of npd_select), and the sequence packer of Algorithm 1
  * (npd_pack_sequences).
  *
+ * Around the step: the LM head's cross-entropy without a teacher (npd_ce_fwd_bwd), the join of a block's
+ * branch with the residual stream and its norms (npd_norm_fwd, npd_norm_bwd), and a linear layer with its
+ * epilogue (npd_linear_fwd, npd_linear_bwd).
+ *
  * Conventions
  *   - Every pointer is a DEVICE pointer unless the comment says HOST.
  *   - The device that holds the buffers, and that the stream belongs to, has to be the current one.
