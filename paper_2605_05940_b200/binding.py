@@ -606,7 +606,7 @@ def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_
                    dw_dtype=torch.bfloat16, dx=None, dw=None, accumulate_dw=False, workspace=None, stream=None):
     """Gradients of npd_linear_fwd from dy bf16 [M, N]: (dx bf16 [M, K], dw [N, K], dbias f32 [N]), None for what
     is not wanted.  preact is the forward's (not needed without an activation), x only for dw.  An f32 dw with
-    accumulate_dw is added to.  The gradient of the residual is dy itself."""
+    accumulate_dw is added to (a new one starts at zero).  The gradient of the residual is dy itself."""
     where = "npd_linear_bwd"
     dev = _device_of(dy, where)
     if dy.dim() != 2 or weight is None or weight.dim() != 2:
@@ -631,6 +631,8 @@ def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_
             a.lddx, a.dx = _matrix(dx, where, dev, (M, K), bf16), dx.data_ptr()
         if dw is None and want_dw:
             dw = _new((N, K), dw_dtype, device)
+            if accumulate_dw:
+                dw.zero_()
         if dw is not None:
             a.lddw, a.dw = _matrix(dw, where, dev, (N, K), dw_dtype), dw.data_ptr()
         dbias = torch.empty(N, dtype=torch.float32, device=device) if want_dbias else None
@@ -699,7 +701,7 @@ class CEStep:
     hidden bf16 [T, d], weight bf16 [V, d], labels int32 [T], loss_mask uint8 or bool [T], token_weight f32 [T].
     norm: a NormJoin that writes `hidden` before, and takes d_hidden back after the step.
     d_hidden / d_weight: True for a new tensor, None for none, or a tensor to write to (an f32 d_weight with
-    accumulate_dw is added to).  The tensors are allocated on `stream` (default: the current one)."""
+    accumulate_dw is added to by every run; a new one starts at zero).  The tensors are allocated on `stream` (default: the current one)."""
 
     def __init__(self, hidden, weight, labels, *, loss_mask=None, token_weight=None, temperature=1.0, grad_scale=1.0,
                  d_hidden=True, d_weight=True, dw_dtype=torch.bfloat16, accumulate_dw=False, want_lse=True,
@@ -730,6 +732,8 @@ class CEStep:
                 d_hidden = _like(hidden, shape, bf16)
             if d_weight is True:
                 d_weight = _new((V, d), dw_dtype, device)
+                if accumulate_dw:
+                    d_weight.zero_()
             self.d_hidden, self.d_weight = d_hidden, d_weight
             if d_hidden is not None:
                 a.ld_dh, a.d_hidden = _matrix(d_hidden, where, dev, shape, bf16), d_hidden.data_ptr()

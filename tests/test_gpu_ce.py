@@ -233,3 +233,18 @@ def test_a_large_case_against_fp64_on_the_gpu():
     P *= (torch.where(on, w.double(), torch.zeros_like(L)) * 1e-3)[:, None]
     rel = lambda a, r: float((a.double() - r).norm() / r.norm())
     assert rel(dH, P @ W) < 3 * u(BF16) and rel(dW, P.t() @ H) < 3 * u(BF16)
+
+
+def test_accumulation_into_a_new_d_weight_starts_at_zero():
+    g = torch.Generator(device=DEV).manual_seed(33)
+    T, d, V = 150, 128, 700
+    H, W = (torch.randn(T, d, device=DEV, generator=g)).to(BF16), (torch.randn(V, d, device=DEV, generator=g) * 0.1).to(BF16)
+    y = torch.randint(0, V, (T,), device=DEV, generator=g, dtype=torch.int32)
+    junk = torch.full((V, d), float("nan"), device=DEV)   # its memory is what the next tensor of this size gets
+    del junk
+    step = B.CEStep(H, W, y, grad_scale=1.0 / T, dw_dtype=torch.float32, accumulate_dw=True)
+    step.run()
+    plain = B.npd_cross_entropy(H, W, y, grad_scale=1.0 / T, dw_dtype=torch.float32)[3]
+    assert torch.equal(step.d_weight, plain)              # one add to zero per element
+    step.run()
+    assert torch.equal(step.d_weight, 2 * plain)          # x + x is exact

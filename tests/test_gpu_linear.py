@@ -233,3 +233,14 @@ def test_plain_product_leaves_what_lies_beyond_its_last_column():
             assert torch.isnan(buf[:, N:]).all()
             bound = u(dt) * np.abs(ref) * 1.01 + 2 * u(F32) * (K / 16 + 16) * (np.abs(host(a)) @ np.abs(host(b)).T)
             assert np.all(np.abs(host(buf[:, :N]) - ref) <= bound)
+
+
+def test_accumulation_into_a_new_dw_starts_at_zero():
+    g = torch.Generator(device=DEV).manual_seed(31)
+    M, N, K = 200, 264, 136
+    dy, x, w = ((torch.randn(s, device=DEV, generator=g)).to(BF16) for s in ((M, N), (M, K), (N, K)))
+    junk = torch.full((N, K), float("nan"), device=DEV)   # its memory is what the next tensor of this size gets
+    del junk
+    _, dw, _ = B.npd_linear_bwd(dy, x, w, want_dx=False, dw_dtype=torch.float32, accumulate_dw=True)
+    _, plain, _ = B.npd_linear_bwd(dy, x, w, want_dx=False, dw_dtype=torch.float32)
+    assert torch.equal(dw, plain)                         # one add to zero per element
