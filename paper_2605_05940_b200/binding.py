@@ -815,9 +815,12 @@ class KDStep:
                                  **self._kw)
 
     def run(self, stream=None):
+        self._run(self.args, stream)
+
+    def _run(self, args, stream):
         if self.norm is not None:
             self.norm.forward(self.batch.hidden, stream)
-        npd_kd_fwd_bwd(self.args, stream)
+        npd_kd_fwd_bwd(args, stream)
         if self.norm is not None and self.d_hidden is not None and self.norm.grads:
             self.norm.backward(self.d_hidden, stream)
 
@@ -839,12 +842,13 @@ class KDStep:
         return evs
 
     def run_recording(self, evs, stream=None):
-        """One step with the library's phase events attached; only enqueues."""
+        """One step with the library's phase events attached; only enqueues.  The join (norm) runs before the
+        first event and after the last."""
         arr = (C.c_void_p * len(evs))(*[e.cuda_event for e in evs])
         a = npd_kd_args.from_buffer_copy(self.args)
         a.phase_events = C.cast(arr, C.POINTER(C.c_void_p))
         a.n_phase_events = len(evs)
-        npd_kd_fwd_bwd(a, stream)
+        self._run(a, stream)
 
     def run_with_phase_times(self, stream=None):
         """One step with the library's phase events attached.  Returns a list of

@@ -124,3 +124,22 @@ def test_one_decoded_token_through_the_tail():
     want = orc.cross_entropy_step(oy, host(weight), label.cpu().numpy())
     bound = 8 * u(BF16) * (np.abs(oy) @ np.abs(host(weight)).T).max()
     assert abs(float(nll) - want[0][0]) <= bound and abs(float(lse) - want[1][0]) <= bound
+
+
+def test_a_timed_step_runs_the_join_too():
+    T, d, V = 200, 128, 904
+    act, w_down, b_down, residual, how = _tail(T, d, 13)
+    b = syn.scaled("c2", device=DEV, T=T, d=d, V=V, min_len=20, max_len=90)
+    b.hidden = torch.zeros((T, d), device=DEV, dtype=BF16)
+    x, _ = B.npd_linear_fwd(act, w_down, bias=b_down)
+    norm = B.NormJoin(x, residual, **how)
+    step = B.KDStep(b, grad_scale=1.0 / b.n_loss, norm=norm)
+    times = step.run_with_phase_times()
+    got = [t.clone() for t in (b.hidden, step.nll_student, step.kl, norm.d_pre_weight)]
+    assert len(times) == len(step.phase_names()) and float(got[0].abs().max()) > 0
+    step.run()
+    torch.cuda.synchronize()
+    for a, c in zip(got[:3], (b.hidden, step.nll_student, step.kl)):
+        assert torch.equal(a, c)
+    # d_hidden's sums over pieces of the vocabulary have no fixed order
+    assert _rel(got[3], host(norm.d_pre_weight)) < 2 * u(BF16)
