@@ -12,9 +12,9 @@
 //
 // Memory bound: every tensor is read once and written once, a row stays in registers between the
 // reduction over it and the result.  A CTA works on one row at a time, eight consecutive elements
-// per thread and vector, and goes on to row + gridDim; the gains stay in registers and the next
-// row's loads are issued before the current row's reductions, so that the memory system has work
-// during the barriers.  The sums over rows (gains, shared gate) are kept per thread over all rows
+// per thread and vector, and goes on to row + gridDim; gains stay in registers as far as they fit, and
+// the next rows' loads are under way during the current row's reductions (the forward holds them in registers, the
+// backward with a bf16 stream in a ring in shared memory).  The sums over rows (gains, shared gate) are kept per thread over all rows
 // of the CTA, written once as a partial row per CTA, and added up in a fixed order by a second
 // kernel: no atomics, the same bits in every run.
 // All arithmetic is fp32; each result is rounded once, when it is stored.  y is taken from the
@@ -58,7 +58,6 @@ constexpr int kMaxD = 16384;
 // registers) in the forward and 4096 (512 threads of 128) in the backward; beyond, two or four vectors per thread
 // (at most 512 of them), gains re-read (they sit in L1/L2), sums over rows in shared memory.
 constexpr int kMaxSmallFwd = 8192, kMaxSmallBwd = 4096;
-constexpr int kMaxThreads = 512;
 constexpr int kMaxSmem = 2 * kMaxD * 4;  // dynamic shared memory a launch may ask for: sums over the widest row
 constexpr int kRing = 2;  // rows in flight per CTA of the backward
 }  // namespace norm_cfg
