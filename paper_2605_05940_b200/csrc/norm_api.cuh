@@ -33,7 +33,8 @@ bool bad_overlap(const Extent& out, const Extent& in, bool in_place) {
 }
 
 struct NormPlan {
-  int vec, threads, smem, grid, part_d;
+  int vec, threads, span, smem, grid, part_d;
+  bool narrow;
   size_t ws;
 };
 
@@ -42,13 +43,17 @@ NormPlan norm_plan(const npd_norm_args* a, int sms, bool backward) {
   NormPlan pl{};
   pl.vec = a->d <= (backward ? kMaxSmallBwd : kMaxSmallFwd) ? 1 : (a->d <= kMaxSmallFwd ? 2 : 4);
   const int per = 8 * pl.vec;
-  pl.threads = ((a->d + per - 1) / per + 31) / 32 * 32;
-  pl.smem = backward && pl.vec > 1 ? 64 * pl.vec * pl.threads : 0;  // sums over rows
+  pl.narrow = a->d <= kNarrowD;
+  pl.threads = pl.narrow ? kNarrowThreads : ((a->d + per - 1) / per + 31) / 32 * 32;
+  pl.span = a->d <= 64 ? 8 : (a->d <= 128 ? 16 : 32);
+  const int rows = pl.narrow ? pl.threads / pl.span : 1;  // of a CTA at a time
+  // sums over rows (and gains up to kMaxSmallFwd), or where the warps' sums meet
+  pl.smem = !backward ? 0 : pl.vec > 1 ? 64 * pl.vec * pl.threads * (pl.vec == 2 ? 2 : 1) : pl.narrow ? 2 * pl.threads * pl.span : 0;
   // Resident CTAs per SM, by threads and (an estimate of) registers: every CTA goes through its share
   // of the rows.  Several per SM, so that one CTA's barriers run under another one's loads.
-  int per_sm = (pl.vec > 1 ? 512 : (!backward ? 1024 : (pl.threads <= 256 ? 816 : 512))) / pl.threads;
+  int per_sm = (backward || pl.vec > 1 ? 512 : 1024) / pl.threads;
   per_sm = std::max(1, std::min(per_sm, 16));
-  pl.grid = std::min(a->T, sms * per_sm);
+  pl.grid = std::min((a->T + rows - 1) / rows, sms * per_sm);
   pl.part_d = (a->d + 3) / 4 * 4;
   pl.ws = align_up(sizeof(float) * 2 * static_cast<size_t>(pl.part_d) * pl.grid, 1024);
   return pl;
@@ -136,8 +141,9 @@ int check_norm(const npd_norm_args* a, bool backward, bool need_pointers) {
   return NPD_OK;
 }
 
-NormParams norm_params(const npd_norm_args* a, bool backward) {
+NormParams norm_params(const npd_norm_args* a, const NormPlan& pl, bool backward) {
   NormParams p{};
+  p.span = pl.span;
   p.T = a->T;
   p.d = a->d;
   p.x = static_cast<const __nv_bfloat16*>(a->x);
@@ -175,13 +181,33 @@ NormParams norm_params(const npd_norm_args* a, bool backward) {
   return p;
 }
 
+using NormKernel = void (*)(NormParams);
+
+// The instances by size of the block, and what the call has (see the kernels).
+template <bool kF32, bool kGate, bool kRagged>
+NormKernel norm_fwd_pick(const NormPlan& pl) {
+  if (pl.narrow) return norm_fwd_kernel<kF32, 1, norm_cfg::kNarrowThreads, kGate, kRagged, true>;
+  return pl.threads <= 512 ? norm_fwd_kernel<kF32, 1, 512, kGate, kRagged, false>
+                           : norm_fwd_kernel<kF32, 1, 1024, kGate, kRagged, false>;
+}
 template <bool kF32>
-void (*norm_bwd_pick(const NormPlan& pl, int form))(NormParams) {
-  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, 0, 512, 1>;
-  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, 0, 512, 1>;
-  if (pl.threads <= 256)
-    return form == 2 ? norm_bwd_kernel<kF32, 1, 2, 256, 3> : form == 1 ? norm_bwd_kernel<kF32, 1, 1, 256, 3> : norm_bwd_kernel<kF32, 1, 0, 256, 2>;
-  return form == 2 ? norm_bwd_kernel<kF32, 1, 2, 512, 1> : form == 1 ? norm_bwd_kernel<kF32, 1, 1, 512, 1> : norm_bwd_kernel<kF32, 1, 0, 512, 1>;
+NormKernel norm_fwd_pick(const NormPlan& pl, bool token_gate, bool ragged) {
+  if (pl.vec > 1) return norm_fwd_kernel<kF32, 4, 512, true, true, false>;
+  if (token_gate) return ragged ? norm_fwd_pick<kF32, true, true>(pl) : norm_fwd_pick<kF32, true, false>(pl);
+  return ragged ? norm_fwd_pick<kF32, false, true>(pl) : norm_fwd_pick<kF32, false, false>(pl);
+}
+template <bool kF32, int kForm, bool kGate>
+NormKernel norm_bwd_pick(const NormPlan& pl) {
+  if (pl.narrow) return norm_bwd_kernel<kF32, 1, kForm, kGate, norm_cfg::kNarrowThreads, true>;
+  return pl.threads <= 256 ? norm_bwd_kernel<kF32, 1, kForm, kGate, 256, false> : norm_bwd_kernel<kF32, 1, kForm, kGate, 512, false>;
+}
+template <bool kF32>
+NormKernel norm_bwd_pick(const NormPlan& pl, int form, bool token_gate) {
+  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, 0, false, 512, false>;
+  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, 0, false, 512, false>;
+  if (form == 0) return norm_bwd_pick<kF32, 0, false>(pl);
+  if (token_gate) return form == 1 ? norm_bwd_pick<kF32, 1, true>(pl) : norm_bwd_pick<kF32, 2, true>(pl);
+  return form == 1 ? norm_bwd_pick<kF32, 1, false>(pl) : form == 2 ? norm_bwd_pick<kF32, 2, false>(pl) : norm_bwd_pick<kF32, 3, false>(pl);
 }
 
 }  // namespace
@@ -207,11 +233,10 @@ int npd_norm_fwd(const npd_norm_args* a, void* cuda_stream) {
   if (di.cc_major != 10) return NPD_EARCH;
   const NormPlan pl = norm_plan(a, di.sms, false);
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
-  auto k = pl.vec > 1          ? (sf ? norm_fwd_kernel<true, 4, 512> : norm_fwd_kernel<false, 4, 512>)
-           : pl.threads <= 512 ? (sf ? norm_fwd_kernel<true, 1, 512> : norm_fwd_kernel<false, 1, 512>)
-                               : (sf ? norm_fwd_kernel<true, 1, 1024> : norm_fwd_kernel<false, 1, 1024>);
+  const bool token_gate = a->gate != nullptr && a->ldg != 0, ragged = a->d % 8 != 0;
+  const NormKernel k = sf ? norm_fwd_pick<true>(pl, token_gate, ragged) : norm_fwd_pick<false>(pl, token_gate, ragged);
   const cudaError_t e = launch_ex(k, pl.grid, pl.threads, 0, static_cast<cudaStream_t>(cuda_stream), false,
-                                  norm_params(a, false));
+                                  norm_params(a, pl, false));
   ++g_launches;
   return e == cudaSuccess ? NPD_OK : NPD_ECUDA;
 }
@@ -224,7 +249,7 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   if ((rc = device_info(&di)) != NPD_OK) return rc;
   if (di.cc_major != 10) return NPD_EARCH;
   const NormPlan pl = norm_plan(a, di.sms, true);
-  NormParams p = norm_params(a, true);
+  NormParams p = norm_params(a, pl, true);
   p.part_d = pl.part_d;
   if (p.want != 0) {
     if (a->workspace == nullptr || (reinterpret_cast<uintptr_t>(a->workspace) & 15u) || a->workspace_bytes < pl.ws)
@@ -233,20 +258,20 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   }
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool full = pl.vec == 1 && a->d % 8 == 0 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr &&
-                    p.dres != nullptr && (p.gate == nullptr || p.ldg == 0);
-  const int form = !full ? 0 : (a->d % 256 == 0 ? 2 : 1);
-  auto k = sf ? norm_bwd_pick<true>(pl, form) : norm_bwd_pick<false>(pl, form);
-  // without the full form's registers fewer CTAs are resident (the workspace is sized for the larger number)
-  const int grid = full ? pl.grid : std::min(pl.grid, di.sms * std::max(1, 512 / pl.threads));
-  const int smem = full && !sf ? norm_cfg::kRing * pl.threads * 16 * 4 : pl.smem;
+  const bool token_gate = p.gate != nullptr && p.ldg != 0;
+  const bool full = pl.vec == 1 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr && p.dres != nullptr &&
+                    (!token_gate || p.dgate != nullptr);
+  const int form = !full ? 0 : a->d % 8 != 0 ? 1 : a->d % 256 != 0 || token_gate ? 2 : 3;
+  const NormKernel k = sf ? norm_bwd_pick<true>(pl, form, token_gate) : norm_bwd_pick<false>(pl, form, token_gate);
+  const int ring = full && !sf ? norm_cfg::kRing * pl.threads * 16 * (token_gate ? 5 : 4) : 0;
+  const int smem = std::max(ring, pl.smem);
   if (smem > 0 && set_smem(k, norm_cfg::kMaxSmem) != NPD_OK) return NPD_ECUDA;
-  cudaError_t e = launch_ex(k, grid, pl.threads, smem, st, false, p);
+  cudaError_t e = launch_ex(k, pl.grid, pl.threads, smem, st, false, p);
   ++g_launches;
   if (e != cudaSuccess) return NPD_ECUDA;
   if (p.want != 0) {
     float* shared_dgate = (p.want & 4) ? static_cast<float*>(a->d_gate) : nullptr;
-    e = launch_dim(norm_sums_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 2), 1024, 0, st, true, p, grid,
+    e = launch_dim(norm_sums_kernel, dim3(static_cast<unsigned>((a->d + 31) / 32), 2), 1024, 0, st, true, p, pl.grid,
                    a->d_pre_weight, a->d_post_weight, shared_dgate);
     ++g_launches;
   }

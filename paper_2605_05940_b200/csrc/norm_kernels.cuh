@@ -50,16 +50,20 @@ struct NormParams {
   float* part;                // [gridDim][2][part_d] partial sums over rows: of dy h r_h, and S (see norm_bwd_kernel)
   int part_d;                 // d rounded up to a multiple of 4
   int want;                   // bit 0: w_pre, bit 1: w_post, bit 2: shared gate
+  int span;                   // narrow rows: threads per row (8, 16 or 32)
 };
 
 namespace norm_cfg {
 constexpr int kMaxD = 16384;
 // One vector of eight per thread, gains (and sums over rows) in registers, up to d = 8192 (1024 threads of 64
 // registers) in the forward and 4096 (512 threads of 128) in the backward; beyond, two or four vectors per thread
-// (at most 512 of them), gains re-read (they sit in L1/L2), sums over rows in shared memory.
+// (at most 512 of them), sums over rows (and up to d = 8192 gains) in shared memory.
 constexpr int kMaxSmallFwd = 8192, kMaxSmallBwd = 4096;
 constexpr int kMaxSmem = 2 * kMaxD * 4;  // dynamic shared memory a launch may ask for: sums over the widest row
 constexpr int kRing = 2;  // rows in flight per CTA of the backward
+// Rows of at most 256 elements lie within a warp (8, 16 or 32 threads each): a block of 256 threads takes several
+// of them at a time, and none of its reductions needs a barrier.
+constexpr int kNarrowD = 256, kNarrowThreads = 256;
 }  // namespace norm_cfg
 
 // ---- eight consecutive elements ----
@@ -70,39 +74,101 @@ template <bool kF32>
 struct Raw8 {
   uint4 q[kF32 ? 2 : 1];
 };
-// Loads elements [c, c+8) of a row, those below d; the others read as 0.  Rows start on 16-byte
-// boundaries and strides are multiples of 16 bytes, so whole vectors are aligned; the last, partial one
-// is fetched element by element (nothing past the row's end is read).
-template <bool kF32>
-__device__ __forceinline__ Raw8<kF32> load8(const void* row, int c, int d) {
-  Raw8<kF32> r;
-  if (c + 8 <= d) {
-    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + static_cast<size_t>(c) * (kF32 ? 4 : 2));
-    r.q[0] = *p;
-    if (kF32) r.q[kF32 ? 1 : 0] = p[1];
-    return r;
-  }
-  uint32_t w[kF32 ? 8 : 4];
-#pragma unroll
-  for (int i = 0; i < (kF32 ? 8 : 4); ++i) {
-    if (kF32) {
-      w[i] = c + i < d ? static_cast<const uint32_t*>(row)[c + i] : 0u;
-    } else {
-      const uint16_t* e = static_cast<const uint16_t*>(row);
-      const uint32_t lo = c + 2 * i < d ? e[c + 2 * i] : 0u, hi = c + 2 * i + 1 < d ? e[c + 2 * i + 1] : 0u;
-      w[i] = lo | (hi << 16);
-    }
-  }
-  r.q[0] = make_uint4(w[0], w[1], w[2], w[3]);
-  if (kF32) r.q[kF32 ? 1 : 0] = make_uint4(w[kF32 ? 4 : 0], w[kF32 ? 5 : 0], w[kF32 ? 6 : 0], w[kF32 ? 7 : 0]);
-  return r;
-}
 template <bool kF32>
 __device__ __forceinline__ Raw8<kF32> zero8() {
   Raw8<kF32> r;
   r.q[0] = make_uint4(0u, 0u, 0u, 0u);
   if (kF32) r.q[kF32 ? 1 : 0] = r.q[0];
   return r;
+}
+// Loads elements [c, c+8) of a row, those below d; the others read as 0.  Rows start on 16-byte boundaries and
+// strides are multiples of 16 bytes, so whole vectors are aligned; the last, partial one is fetched in pieces of
+// four, two and one elements (nothing past the row's end is read).
+template <bool kF32>
+__device__ __forceinline__ Raw8<kF32> load8(const void* row, int c, int d) {
+  Raw8<kF32> r;
+  const int n = d - c;
+  const char* at = static_cast<const char*>(row) + static_cast<size_t>(c) * (kF32 ? 4 : 2);
+  if (n >= 8) {
+    r.q[0] = *reinterpret_cast<const uint4*>(at);
+    if (kF32) r.q[kF32 ? 1 : 0] = reinterpret_cast<const uint4*>(at)[1];
+    return r;
+  }
+  r = zero8<kF32>();
+  if (n <= 0) return r;
+  if (kF32) {
+    const uint32_t* e = reinterpret_cast<const uint32_t*>(at);
+    uint4 tail = make_uint4(0u, 0u, 0u, 0u);  // the last n % 4
+    const uint32_t* f = e + (n & 4);
+    if (n & 2) {
+      const uint2 u = *reinterpret_cast<const uint2*>(f);
+      tail.x = u.x;
+      tail.y = u.y;
+      if (n & 1) tail.z = f[2];
+    } else if (n & 1) {
+      tail.x = f[0];
+    }
+    if (n & 4) {
+      r.q[0] = *reinterpret_cast<const uint4*>(e);
+      r.q[kF32 ? 1 : 0] = tail;
+    } else {
+      r.q[0] = tail;
+    }
+  } else {
+    uint32_t lo = 0u, hi = 0u;  // the last n % 4
+    const uint16_t* f = reinterpret_cast<const uint16_t*>(at) + (n & 4);
+    if (n & 2) {
+      lo = *reinterpret_cast<const uint32_t*>(f);
+      if (n & 1) hi = f[2];
+    } else if (n & 1) {
+      lo = f[0];
+    }
+    if (n & 4) {
+      const uint2 u = *reinterpret_cast<const uint2*>(at);
+      r.q[0] = make_uint4(u.x, u.y, lo, hi);
+    } else {
+      r.q[0] = make_uint4(lo, hi, 0u, 0u);
+    }
+  }
+  return r;
+}
+// The same for a prefetch, which must not touch what it loads: whole 16-byte pieces with an element of the row in
+// them (n = d - c elements are left of it).  A piece that also reaches past the row's end lies in the row's own stride,
+// but for the last row, whose partial piece is left out; trim8 brings a partial vector in order when it is used.
+template <bool kF32, bool kRagged>
+__device__ __forceinline__ Raw8<kF32> fetch8(const void* row, int c, int n, bool last) {
+  Raw8<kF32> r = zero8<kF32>();
+  const uint4* at = reinterpret_cast<const uint4*>(static_cast<const char*>(row) + static_cast<size_t>(c) * (kF32 ? 4 : 2));
+  constexpr int kPer = kF32 ? 4 : 8;
+  const int over = kRagged && last ? kPer - 1 : 0;
+  if (n > over) r.q[0] = at[0];
+  if (kF32) {
+    if (n > (kRagged ? kPer + over : 0)) r.q[kF32 ? 1 : 0] = at[1];
+  }
+  return r;
+}
+// For 0 < d - c < 8.
+template <bool kF32>
+__device__ __forceinline__ void trim8(Raw8<kF32>& r, const void* row, int c, int d, bool last) {
+  if (last) {
+    r = load8<kF32>(row, c, d);
+    return;
+  }
+  const int n = d - c;
+  if (kF32) {
+    uint4& a = r.q[0];
+    uint4& b = r.q[kF32 ? 1 : 0];
+    a.y = n > 1 ? a.y : 0u;
+    a.z = n > 2 ? a.z : 0u;
+    a.w = n > 3 ? a.w : 0u;
+    b.x = n > 4 ? b.x : 0u;
+    b.y = n > 5 ? b.y : 0u;
+    b.z = n > 6 ? b.z : 0u;
+    b.w = 0u;
+  } else {
+    auto keep = [&](uint32_t w, int i) { return n > i + 1 ? w : (n > i ? w & 0xffffu : 0u); };
+    r.q[0] = make_uint4(keep(r.q[0].x, 0), keep(r.q[0].y, 2), keep(r.q[0].z, 4), keep(r.q[0].w, 6));
+  }
 }
 template <bool kF32>
 __device__ __forceinline__ V8 unpack8(const Raw8<kF32>& r) {
@@ -122,27 +188,32 @@ __device__ __forceinline__ V8 unpack8(const Raw8<kF32>& r) {
   }
   return o;
 }
-template <bool kF32>
+// Stores them, those below d (kRagged: d may lie inside the vector).
+template <bool kF32, bool kRagged = true>
 __device__ __forceinline__ void store8(void* row, int c, int d, const V8& a) {
+  const int n = kRagged ? d - c : (c < d ? 8 : 0);
   if (kF32) {
     float* p = static_cast<float*>(row) + c;
-    if (c + 8 <= d) {
+    if (n >= 8) {
       reinterpret_cast<float4*>(p)[0] = make_float4(a.v[0], a.v[1], a.v[2], a.v[3]);
       reinterpret_cast<float4*>(p)[1] = make_float4(a.v[4], a.v[5], a.v[6], a.v[7]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < d) p[i] = a.v[i];
+    } else if (n > 0) {
+      if (n & 4) *reinterpret_cast<float4*>(p) = make_float4(a.v[0], a.v[1], a.v[2], a.v[3]);
+      float* f = p + (n & 4);
+      if (n & 2) *reinterpret_cast<float2*>(f) = n & 4 ? make_float2(a.v[4], a.v[5]) : make_float2(a.v[0], a.v[1]);
+      if (n & 1) p[n - 1] = n & 4 ? (n & 2 ? a.v[6] : a.v[4]) : (n & 2 ? a.v[2] : a.v[0]);
     }
   } else {
     __nv_bfloat16* p = static_cast<__nv_bfloat16*>(row) + c;
-    if (c + 8 <= d) {
-      *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(a.v[0], a.v[1]), pack_bf16x2(a.v[2], a.v[3]),
-                                                pack_bf16x2(a.v[4], a.v[5]), pack_bf16x2(a.v[6], a.v[7]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (c + i < d) p[i] = __float2bfloat16_rn(a.v[i]);
+    const uint32_t w[4] = {pack_bf16x2(a.v[0], a.v[1]), pack_bf16x2(a.v[2], a.v[3]), pack_bf16x2(a.v[4], a.v[5]),
+                           pack_bf16x2(a.v[6], a.v[7])};
+    if (n >= 8) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else if (n > 0) {
+      if (n & 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+      const uint32_t lo = n & 4 ? w[2] : w[0], hi = n & 4 ? w[3] : w[1];  // the last n % 4
+      if (n & 2) *reinterpret_cast<uint32_t*>(p + (n & 4)) = lo;
+      if (n & 1) reinterpret_cast<uint16_t*>(p)[n - 1] = static_cast<uint16_t>(n & 2 ? hi : lo);
     }
   }
 }
@@ -212,7 +283,7 @@ template <bool kF32>
 __device__ __forceinline__ P8 pairs8(const Raw8<kF32>& r) {
   return pack8(unpack8<kF32>(r));
 }
-template <bool kF32>
+template <bool kF32, bool kRagged = true>
 __device__ __forceinline__ void store8(void* row, int c, int d, const P8& a) {
   V8 v;
 #pragma unroll
@@ -221,13 +292,14 @@ __device__ __forceinline__ void store8(void* row, int c, int d, const P8& a) {
     v.v[2 * i] = q.x;
     v.v[2 * i + 1] = q.y;
   }
-  store8<kF32>(row, c, d, v);
+  store8<kF32, kRagged>(row, c, d, v);
 }
 
 // ---- a ring of rows in shared memory, filled by asynchronous copies; slot s of a stage holds 16 bytes of every
 // thread, and every thread copies and reads only its own, so the ring needs no barrier ----
-__device__ __forceinline__ void async_copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// 16 bytes, of which the first `bytes` are read and the others filled with zeros.
+__device__ __forceinline__ void async_copy16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // Waits until at most kPending of this thread's newest groups are in flight.
@@ -253,9 +325,18 @@ __device__ __forceinline__ void clear_sums(SumBuf<N>* buf, int count) {
   float* f = reinterpret_cast<float*>(buf);
   for (int i = threadIdx.x; i < count * N * 32; i += blockDim.x) f[i] = 0.f;
 }
-// kWide: the block may have more than 16 warps.
-template <int N, bool kWide = false>
-__device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
+// kWide: the block may have more than 16 warps.  kNarrow: sums over `span` neighbouring threads instead, without a barrier.
+template <int N, bool kWide, bool kNarrow>
+__device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf, int span) {
+  if (kNarrow) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      if (o >= 8 && o >= span) continue;  // the same for the whole grid
+#pragma unroll
+      for (int k = 0; k < N; ++k) s[k] += __shfl_xor_sync(0xffffffffu, s[k], o);
+    }
+    return;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
 #pragma unroll
   for (int k = 0; k < N; ++k) s[k] = warp_sum(s[k]);
@@ -283,20 +364,30 @@ __device__ __forceinline__ void block_sum(float (&s)[N], SumBuf<N>& buf) {
 // What is missing in a call costs no branches in the arithmetic: a missing gain or gate is a gain of 1, a
 // missing operand zeros, and a branch without a norm has r_x = 1.
 
-// Forward.  kVec vectors of eight per thread; vector j of a thread starts at 8 * (threadIdx + j * blockDim).
-template <bool kF32, int kVec, int kThreads>
+// Forward.  kVec vectors of eight per thread; vector j of a thread starts at 8 * (its number in the row + j * blockDim).
+// kGate: with kVec == 1 every token has a gate of its own (else none has); otherwise the call says.  kRagged: d need
+// not be a multiple of 8.  Neither is carried along where it is not needed (d = 728, T = 65,536, bf16: 69 us; with the
+// tests for a ragged row 87 us, with both decided at run time 94 us).  kNarrow: see norm_cfg (d = 64, T = 65,536:
+// 8.2 us; a block of one warp per row took 40 us).
+template <bool kF32, int kVec, int kThreads, bool kGate, bool kRagged, bool kNarrow>
 __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) norm_fwd_kernel(const NormParams p) {
   __shared__ SumBuf<1> red[4];
   constexpr bool kHold = kVec == 1;  // gains held in registers, the next row's loads in flight
+  constexpr bool kWide = kThreads > 512;
+  // 1024 threads of 64 registers do not hold an fp32 row with its gate and the next ones: only x comes a row ahead,
+  // gate and residual with the row (d = 8192, T = 10,000: 188 us; all of it ahead, with spills, 255 us)
+  constexpr bool kLate = kHold && kWide && kF32 && kGate;
   constexpr size_t es = kF32 ? 4 : 2;
   const int nt = blockDim.x;
+  const int span = kNarrow ? p.span : nt, sub = kNarrow ? static_cast<int>(threadIdx.x) / span : 0, rows = kNarrow ? nt / span : 1;
+  const int col0 = 8 * (static_cast<int>(threadIdx.x) - sub * span);
   const float inv_d = 1.f / static_cast<float>(p.d);
-  const bool token_gate = p.gate != nullptr && p.ldg != 0;
+  const bool token_gate = kGate && (kHold || (p.gate != nullptr && p.ldg != 0));
   P8 wp[kVec], wq[kVec];  // gain of the branch times a shared gate; gain of y
   grid_dependency_wait();
   grid_launch_dependents();
   auto gains = [&](int j) {
-    const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+    const int c = col0 + 8 * j * nt;
     V8 w = gain8<!kHold>(p.w_post, p.w_f32, p.offset, c, p.d);
     if (p.gate != nullptr && !token_gate) {
       const V8 g = unpack8<false>(load8<false>(p.gate, c, p.d));
@@ -307,31 +398,53 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
     wq[j] = pack8(gain8<!kHold>(p.w_pre, p.w_f32, p.offset, c, p.d));
   };
   if (kHold) gains(0);
-  clear_sums(red, 4);
-  __syncthreads();
+  if (!kNarrow) {
+    clear_sums(red, 4);
+    __syncthreads();
+  }
   struct Row {
     Raw8<false> x[kVec], g[kVec];
     Raw8<kF32> r[kVec];
   };
+  auto x_row = [&](int t) { return p.x + static_cast<size_t>(t) * p.ldx; };
+  auto r_row = [&](int t) { return static_cast<const char*>(p.residual) + static_cast<size_t>(t) * p.ldr * es; };
+  auto g_row = [&](int t) { return p.gate + static_cast<size_t>(t) * p.ldg; };
   auto fetch = [&](int t) {
     Row o;
+    const bool last = t == p.T - 1;
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      o.x[j] = p.x != nullptr ? load8<false>(p.x + static_cast<size_t>(t) * p.ldx, c, p.d) : zero8<false>();
-      o.r[j] = p.residual != nullptr
-                  ? load8<kF32>(static_cast<const char*>(p.residual) + static_cast<size_t>(t) * p.ldr * es, c, p.d)
-                  : zero8<kF32>();
-      if (token_gate) o.g[j] = load8<false>(p.gate + static_cast<size_t>(t) * p.ldg, c, p.d);
+      const int c = col0 + 8 * j * nt, n = kNarrow && t >= p.T ? 0 : p.d - c;
+      o.x[j] = p.x != nullptr ? fetch8<false, kRagged>(x_row(t), c, n, last) : zero8<false>();
+      if (!kLate) o.r[j] = p.residual != nullptr ? fetch8<kF32, kRagged>(r_row(t), c, n, last) : zero8<kF32>();
+      if (token_gate && !kLate) o.g[j] = fetch8<false, kRagged>(g_row(t), c, n, last);
     }
     return o;
   };
-  int t = blockIdx.x, par = 0;
+  const int step = static_cast<int>(gridDim.x) * rows;
+  int par = 0;
   Row next;
-  if (kHold && t < p.T) next = fetch(t);
-  for (; t < p.T; t += gridDim.x, par ^= 1) {
-    const Row cur = kHold ? next : fetch(t);
-    if (kHold && t + static_cast<int>(gridDim.x) < p.T) next = fetch(t + gridDim.x);
+  if (kHold && static_cast<int>(blockIdx.x) * rows < p.T) next = fetch(static_cast<int>(blockIdx.x) * rows + sub);
+  for (int t0 = static_cast<int>(blockIdx.x) * rows; t0 < p.T; t0 += step, par ^= 1) {
+    const int t = t0 + sub;
+    const int lim = kNarrow && t >= p.T ? 0 : p.d;  // columns below it are stored
+    Row cur = kHold ? next : fetch(t);
+    if (kLate) {
+      cur.g[0] = fetch8<false, kRagged>(g_row(t), col0, p.d - col0, t == p.T - 1);
+      cur.r[0] = p.residual != nullptr ? fetch8<kF32, kRagged>(r_row(t), col0, p.d - col0, t == p.T - 1) : zero8<kF32>();
+    }
+    if (kHold && t0 + step < p.T) next = fetch(t + step);
+    if (kRagged) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) {
+        const int c = col0 + 8 * j * nt;
+        if (c >= lim || c + 8 <= lim) continue;
+        const bool last = t == p.T - 1;
+        if (p.x != nullptr) trim8<false>(cur.x[j], x_row(t), c, p.d, last);
+        if (p.residual != nullptr) trim8<kF32>(cur.r[j], r_row(t), c, p.d, last);
+        if (token_gate) trim8<false>(cur.g[j], g_row(t), c, p.d, last);
+      }
+    }
     float scale = p.branch_scale;
     if (p.post) {
       unsigned long long q = 0ull;
@@ -342,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
         for (int i = 0; i < 4; ++i) q = fma2(x.p[i], x.p[i], q);
       }
       float s[1] = {sum2(q)};
-      block_sum<1, (kThreads > 512)>(s, red[2 * par]);
+      block_sum<1, kWide, kNarrow>(s, red[2 * par], span);
       scale *= rsqrtf(fmaf(s[0], inv_d, p.eps));
     }
     const unsigned long long scale2 = pair2(scale, scale), res2 = pair2(p.res_scale, p.res_scale);
@@ -350,7 +463,7 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
     P8 h[kVec];
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+      const int c = col0 + 8 * j * nt;
       if (!kHold) gains(j);
       const P8 x = pairs8<false>(cur.x[j]), r = pairs8<kF32>(cur.r[j]);
       P8 w = wp[j];
@@ -365,49 +478,57 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
         h[j].p[i] = fma2(res2, r.p[i], b);
         q = fma2(h[j].p[i], h[j].p[i], q);
       }
-      if (p.h != nullptr) store8<kF32>(static_cast<char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, p.d, h[j]);
+      if (p.h != nullptr)
+        store8<kF32, kRagged>(static_cast<char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, lim, h[j]);
     }
     if (p.y == nullptr) continue;
     float s[1] = {sum2(q)};
-    block_sum<1, (kThreads > 512)>(s, red[2 * par + 1]);
+    block_sum<1, kWide, kNarrow>(s, red[2 * par + 1], span);
     const float rh = rsqrtf(fmaf(s[0], inv_d, p.eps));
     const unsigned long long rh2 = pair2(rh, rh);
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
       P8 o;
 #pragma unroll
       for (int i = 0; i < 4; ++i) o.p[i] = mul2(mul2(h[j].p[i], rh2), wq[j].p[i]);
-      store8<false>(p.y + static_cast<size_t>(t) * p.ldy, c, p.d, o);
+      store8<false, kRagged>(p.y + static_cast<size_t>(t) * p.ldy, col0 + 8 * j * nt, lim, o);
     }
   }
 }
 
 // Backward.  With G = b gate gain_post, v = dh G, and the sums over rows behind the gains and a shared gate are
 // d_post = b gate S and d_gate = b gain_post S with the same S = sum_t dh x r_x (times the row's gate, if
-// every token has its own), so a column needs two sums and two gains: they stay in registers with kVec == 1
-// (80 registers, four CTAs of 192 threads per SM at d = 1536: enough warps to cover each other's reductions
-// and loads; with prefetched rows as well, three warps per scheduler waited for their own shuffles, and with
-// gains in shared memory that memory's pipe was the limit).  Otherwise the sums are in shared memory
-// (dynamic, [2][d]) and gains are re-read.
-// kForm > 0: every operand and result exists, no per-token gate, d a multiple of 8 (no vector is partly outside the
-// row); 2: of 256 (no thread is outside it): the same arithmetic without the tests for it (d = 1536 with form 1:
-// 230 us instead of 198 at T = 65,536; d = 1000 with form 0: 78 us instead of 50 at T = 16,384).  With a bf16 stream rows then arrive
-// through a ring of kRing stages in shared memory (asynchronous copies, two rows ahead), so that loads are in
-// flight during the reductions without taking registers: T = 65,536, d = 1536 takes 198 us with it and 259 us
-// without.  With an fp32 stream the ring is slower (387 us against 315 us).
-template <bool kF32, int kVec, int kForm, int kThreads, int kBlocks>
-__global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormParams p) {
+// every token has its own), so a column needs two sums and two gains.  kVec == 1: they stay in registers, and the
+// next rows' loads are in flight during the reductions: with a bf16 stream in a ring of kRing stages in shared memory
+// (asynchronous copies, which take no registers), with an fp32 stream the next row in registers (d = 4096, T = 20,000:
+// 252 us with it, 347 without; a ragged row is faster without, d = 300: 107 us against 120).  That
+// takes up to 128 registers and leaves 512 threads per SM, which is enough once the loads are ahead: cut down to 80
+// registers for 768 threads, the kernel spills (d = 1536, T = 53,328, bf16: 212 us against 167).
+// kVec == 2: sums and gains in shared memory (dynamic, [2][d] each; d = 8192, T = 10,000: 254 us, with the gains read
+// from memory and put together for each row 338 us; rows in a ring as well: no faster, so it is not the loads
+// that they wait for).  kVec == 4: only the sums fit, gains are re-read.
+// kForm > 0: every operand and result exists, and with kGate every token has its own gate (without it none has).  2: d
+// is a multiple of 8 besides (no vector is partly outside the row); 3: of 256 (no thread is; d = 2048, T = 40,000: 160 us,
+// as form 2 172 us, as form 1 170; an fp32 stream as form 1 296 us instead of 228).  A call with a missing part takes
+// form 0, which tests for it (a per-token gate at d = 1536, T = 53,328: 372 us in form 0, 202 us in its own).
+// kNarrow: see norm_cfg (d = 128, T = 65,536, bf16: 23 us; a block of one warp per row took 41 us).
+template <bool kF32, int kVec, int kForm, bool kGate, int kThreads, bool kNarrow>
+__global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_kernel(const NormParams p) {
   __shared__ SumBuf<3> red3[2];
   __shared__ SumBuf<1> red1[2];
   extern __shared__ __align__(16) float dyn[];  // sums over rows, or the ring
-  constexpr bool kHold = kVec == 1, kFull = kForm > 0;
-  constexpr int kRing = norm_cfg::kRing;
+  constexpr bool kHold = kVec == 1, kFull = kForm > 0, kRagged = kForm < 2;
   constexpr bool kRows = kFull && !kF32;  // rows arrive through the ring
+  constexpr bool kKept = kVec == 2;       // gains kept in shared memory
+  constexpr int kRing = norm_cfg::kRing;
+  constexpr bool kNext = kFull && kF32 && !kRagged;  // the next row is in flight in registers
   constexpr size_t es = kF32 ? 4 : 2;
   const int nt = blockDim.x;
+  const int span = kNarrow ? p.span : nt, sub = kNarrow ? static_cast<int>(threadIdx.x) / span : 0, rows = kNarrow ? nt / span : 1;
+  const int col0 = 8 * (static_cast<int>(threadIdx.x) - sub * span);
   const float inv_d = 1.f / static_cast<float>(p.d);
-  const bool shared_gate = p.gate != nullptr && p.ldg == 0, token_gate = !kFull && p.gate != nullptr && p.ldg != 0;
+  const bool shared_gate = !(kFull && kGate) && p.gate != nullptr && p.ldg == 0;
+  const bool token_gate = kFull ? kGate : p.gate != nullptr && p.ldg != 0;
   const bool have_y = kFull || p.dy != nullptr, have_dh = kFull || p.dh != nullptr, have_x = kFull || p.x != nullptr;
   P8 acc[2];  // kHold: sums over this CTA's rows of dy h r_h and of dh x r_x
   P8 held[2];  // kHold: gain of y, G
@@ -425,66 +546,96 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
   };
   // !kHold: the sums, [sum][vector][half] planes of 16 bytes per thread
   ulonglong2* sums = reinterpret_cast<ulonglong2*>(dyn);
+  ulonglong2* kept = sums + 4 * kVec * nt;  // kKept: the gains, in the same order
   auto gain = [&](int which, int j) {
-    return kHold ? held[which] : read_gain(which, 8 * (static_cast<int>(threadIdx.x) + j * nt));
+    if (kHold) return held[which];
+    if (!kKept) return read_gain(which, col0 + 8 * j * nt);
+    P8 o;
+    const ulonglong2* q = kept + 2 * (which * kVec + j) * nt + threadIdx.x;
+    const ulonglong2 lo = q[0], hi = q[nt];
+    o.p[0] = lo.x;
+    o.p[1] = lo.y;
+    o.p[2] = hi.x;
+    o.p[3] = hi.y;
+    return o;
   };
-  clear_sums(red3, 2);
-  clear_sums(red1, 2);
+  if (!kNarrow) {
+    clear_sums(red3, 2);
+    clear_sums(red1, 2);
+  }
   grid_dependency_wait();
   if (kHold) {
-    held[0] = read_gain(0, 8 * static_cast<int>(threadIdx.x));
-    held[1] = read_gain(1, 8 * static_cast<int>(threadIdx.x));
+    held[0] = read_gain(0, col0);
+    held[1] = read_gain(1, col0);
   } else {
     // every thread clears, adds to and reads back its own columns only: no barrier needed
     for (int i = 0; i < 4 * kVec; ++i) sums[i * nt + threadIdx.x] = make_ulonglong2(0ull, 0ull);
+    if (kKept) {
+#pragma unroll
+      for (int w = 0; w < 2 * kVec; ++w) {
+        const P8 v = read_gain(w / kVec, col0 + 8 * (w % kVec) * nt);
+        for (int half = 0; half < 2; ++half)
+          kept[(2 * w + half) * nt + threadIdx.x] = make_ulonglong2(v.p[2 * half], v.p[2 * half + 1]);
+      }
+    }
   }
-  __syncthreads();
+  if (!kNarrow) __syncthreads();
   struct Row {
     Raw8<false> dy[kVec], x[kVec], g[kVec];
     Raw8<kF32> h[kVec], dh[kVec];
   };
-  const int d_ = kFull ? 1 << 30 : p.d;  // kFull: no vector reaches past the row ...
-  const bool active = kForm != 1 || 8 * static_cast<int>(threadIdx.x) < p.d;  // ... and threads beyond it hold zeros
+  auto dy_row = [&](int t) { return p.dy + static_cast<size_t>(t) * p.lddy; };
+  auto x_row = [&](int t) { return p.x + static_cast<size_t>(t) * p.ldx; };
+  auto g_row = [&](int t) { return p.gate + static_cast<size_t>(t) * p.ldg; };
+  auto h_row = [&](int t) { return static_cast<const char*>(p.h) + static_cast<size_t>(t) * p.ldh * es; };
+  auto dh_row = [&](int t) { return static_cast<const char*>(p.dh) + static_cast<size_t>(t) * p.lddh * es; };
+  const bool active = kForm == 3 || col0 < p.d;  // kHold: this thread has columns of the row
   auto fetch = [&](int t) {
     Row o;
-    if (!active) {
-      o.dy[0] = o.x[0] = zero8<false>();
-      o.h[0] = o.dh[0] = zero8<kF32>();
-      return o;
-    }
+    const bool last = t == p.T - 1;
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
-      if (have_y) {
-        o.dy[j] = load8<false>(p.dy + static_cast<size_t>(t) * p.lddy, c, d_);
-        o.h[j] = load8<kF32>(static_cast<const char*>(p.h) + static_cast<size_t>(t) * p.ldh * es, c, d_);
-      } else {
-        o.dy[j] = zero8<false>();
-        o.h[j] = zero8<kF32>();
-      }
-      o.dh[j] = have_dh ? load8<kF32>(static_cast<const char*>(p.dh) + static_cast<size_t>(t) * p.lddh * es, c, d_) : zero8<kF32>();
-      o.x[j] = have_x ? load8<false>(p.x + static_cast<size_t>(t) * p.ldx, c, d_) : zero8<false>();
-      if (token_gate) o.g[j] = load8<false>(p.gate + static_cast<size_t>(t) * p.ldg, c, d_);
+      const int c = col0 + 8 * j * nt, n = kNarrow && t >= p.T ? 0 : (kForm == 3 ? 8 : p.d - c);
+      o.dy[j] = have_y ? fetch8<false, kRagged>(dy_row(t), c, n, last) : zero8<false>();
+      o.h[j] = have_y ? fetch8<kF32, kRagged>(h_row(t), c, n, last) : zero8<kF32>();
+      o.dh[j] = have_dh ? fetch8<kF32, kRagged>(dh_row(t), c, n, last) : zero8<kF32>();
+      o.x[j] = have_x ? fetch8<false, kRagged>(x_row(t), c, n, last) : zero8<false>();
+      if (token_gate) o.g[j] = fetch8<false, kRagged>(g_row(t), c, n, last);
     }
     return o;
   };
-  // the ring: slots of a stage are dy, x, h, dh
-  constexpr int kSlots = 4;
+  auto trim = [&](Row& o, int t) {
+    const bool last = t == p.T - 1;
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const int c = col0 + 8 * j * nt;
+      if (c >= p.d || c + 8 <= p.d || (kNarrow && t >= p.T)) continue;
+      if (have_y) trim8<false>(o.dy[j], dy_row(t), c, p.d, last);
+      if (have_y) trim8<kF32>(o.h[j], h_row(t), c, p.d, last);
+      if (have_dh) trim8<kF32>(o.dh[j], dh_row(t), c, p.d, last);
+      if (have_x) trim8<false>(o.x[j], x_row(t), c, p.d, last);
+      if (token_gate) trim8<false>(o.g[j], g_row(t), c, p.d, last);
+    }
+  };
+  // the ring: slots of a stage are dy, x, h, dh and a per-token gate
+  constexpr int kSlots = kGate ? 5 : 4;
   const uint32_t slot = 16u * static_cast<uint32_t>(nt), ring0 = smem_u32(dyn) + 16u * threadIdx.x;
+  const uint32_t bytes = kRagged ? static_cast<uint32_t>(min(16, 2 * (p.d - col0))) : 16u;
   auto issue = [&](int t, int stage) {
     if (t < p.T && active) {
       const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
-      async_copy16(at, p.dy + static_cast<size_t>(t) * p.lddy + 8 * threadIdx.x);
-      async_copy16(at + slot, p.x + static_cast<size_t>(t) * p.ldx + 8 * threadIdx.x);
-      async_copy16(at + 2 * slot, static_cast<const __nv_bfloat16*>(p.h) + static_cast<size_t>(t) * p.ldh + 8 * threadIdx.x);
-      async_copy16(at + 3 * slot, static_cast<const __nv_bfloat16*>(p.dh) + static_cast<size_t>(t) * p.lddh + 8 * threadIdx.x);
+      async_copy16(at, dy_row(t) + col0, bytes);
+      async_copy16(at + slot, x_row(t) + col0, bytes);
+      async_copy16(at + 2 * slot, h_row(t) + 2 * col0, bytes);
+      async_copy16(at + 3 * slot, dh_row(t) + 2 * col0, bytes);
+      if (kGate) async_copy16(at + 4 * slot, g_row(t) + col0, bytes);
     }
     async_commit();
   };
-  auto take = [&](int stage) {
+  auto take = [&](int stage, bool on) {
     Row o;
-    if (!active) {
-      o.dy[0].q[0] = o.x[0].q[0] = o.h[0].q[0] = o.dh[0].q[0] = make_uint4(0u, 0u, 0u, 0u);
+    if (!on) {
+      o.dy[0].q[0] = o.x[0].q[0] = o.h[0].q[0] = o.dh[0].q[0] = o.g[0].q[0] = make_uint4(0u, 0u, 0u, 0u);
       return o;
     }
     const uint32_t at = ring0 + static_cast<uint32_t>(stage) * kSlots * slot;
@@ -492,19 +643,28 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     o.x[0].q[0] = ring_get(at + slot);
     o.h[0].q[0] = ring_get(at + 2 * slot);
     o.dh[0].q[0] = ring_get(at + 3 * slot);
+    if (kGate) o.g[0].q[0] = ring_get(at + 4 * slot);
     return o;
   };
   const unsigned long long rs2 = pair2(p.res_scale, p.res_scale);
+  const int step = static_cast<int>(gridDim.x) * rows;
   int par = 0, stage = 0;
-  if (kRows)
-    for (int i = 0; i < kRing; ++i) issue(blockIdx.x + i * static_cast<int>(gridDim.x), i);
-  for (int t = blockIdx.x; t < p.T; t += gridDim.x, par ^= 1) {
+#pragma unroll
+  for (int i = 0; i < (kRows ? kRing : 0); ++i) issue(static_cast<int>(blockIdx.x) * rows + sub + i * step, i);
+  Row next;
+  if (kNext && static_cast<int>(blockIdx.x) * rows < p.T) next = fetch(static_cast<int>(blockIdx.x) * rows + sub);
+  for (int t0 = static_cast<int>(blockIdx.x) * rows; t0 < p.T; t0 += step, par ^= 1) {
+    const int t = t0 + sub;
+    const bool on = active && (!kNarrow || t < p.T);
+    const int lim = kNarrow && t >= p.T ? 0 : (kForm == 3 ? 1 << 30 : p.d);  // columns below it are stored
     Row cur;
     if (kRows) {
       async_wait<kRing - 1>();
-      cur = take(stage);
+      cur = take(stage, on);
     } else {
-      cur = fetch(t);
+      cur = kNext ? next : fetch(t);
+      if (kNext && t0 + step < p.T) next = fetch(t + step);
+      if (kRagged) trim(cur, t);
     }
     P8 vv[kVec];
     unsigned long long s0 = 0ull, s1 = 0ull, s2 = 0ull;
@@ -520,11 +680,11 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     }
     if (kRows) {
       // the stage's values are in registers: its place is free for the row kRing further on
-      issue(t + kRing * static_cast<int>(gridDim.x), stage);
+      issue(t + kRing * step, stage);
       stage = stage + 1 == kRing ? 0 : stage + 1;
     }
     float s[3] = {sum2(s0), sum2(s1), sum2(s2)};  // sum h^2, sum g h, sum x^2
-    block_sum<3>(s, red3[par]);
+    block_sum<3, false, kNarrow>(s, red3[par], span);
     const float rh = have_y ? rsqrtf(fmaf(s[0], inv_d, p.eps)) : 0.f;
     const float rx = p.post ? rsqrtf(fmaf(s[2], inv_d, p.eps)) : 1.f;
     const float ch = -rh * rh * s[1] * inv_d;
@@ -532,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
     unsigned long long q = 0ull;  // sum v x
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt);
+      const int c = col0 + 8 * j * nt;
       const P8 dy = pairs8<false>(cur.dy[j]), h = pairs8<kF32>(cur.h[j]), x = pairs8<false>(cur.x[j]),
                dh = pairs8<kF32>(cur.dh[j]);
       const P8 wq = gain(0, j), G = gain(1, j);
@@ -552,8 +712,10 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
         q = fma2(v, x.p[i], q);
         vv[j].p[i] = v;
         if (kHold) {
-          acc[0].p[i] = fma2(mul2(dy.p[i], h.p[i]), rh2, acc[0].p[i]);
-          acc[1].p[i] = fma2(d2, xn, acc[1].p[i]);
+          if (!kNarrow || on) {  // a row beyond the last: its zeros times a reciprocal norm need not be zeros (eps = 0)
+            acc[0].p[i] = fma2(mul2(dy.p[i], h.p[i]), rh2, acc[0].p[i]);
+            acc[1].p[i] = fma2(d2, xn, acc[1].p[i]);
+          }
         } else {
           a0.p[i] = mul2(dy.p[i], h.p[i]);
           a1.p[i] = xn;
@@ -570,14 +732,15 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
           *w = make_ulonglong2(fma2(d2s.p[2 * half], a1.p[2 * half], sw.x), fma2(d2s.p[2 * half + 1], a1.p[2 * half + 1], sw.y));
         }
       }
-      if (kFull ? active : p.dres != nullptr)
-        store8<kF32>(static_cast<char*>(p.dres) + static_cast<size_t>(t) * p.lddres * es, c, d_, o);
-      if (token_gate && p.dgate != nullptr) store8<false>(p.dgate + static_cast<size_t>(t) * p.lddgate, c, d_, dg);
+      if (kFull || p.dres != nullptr)
+        store8<kF32, kRagged>(static_cast<char*>(p.dres) + static_cast<size_t>(t) * p.lddres * es, c, lim, o);
+      if (token_gate && (kFull || p.dgate != nullptr))
+        store8<false, kRagged>(p.dgate + static_cast<size_t>(t) * p.lddgate, c, lim, dg);
     }
     if (!kFull && p.dx == nullptr) continue;
     if (p.post) {
       float sq[1] = {sum2(q)};
-      block_sum<1>(sq, red1[par]);
+      block_sum<1, false, kNarrow>(sq, red1[par], span);
       const float cx = -rx * rx * sq[0] * inv_d;
       const unsigned long long cx2 = pair2(cx, cx);
 #pragma unroll
@@ -587,29 +750,62 @@ __global__ void __launch_bounds__(kThreads, kBlocks) norm_bwd_kernel(const NormP
         for (int i = 0; i < 4; ++i) vv[j].p[i] = mul2(rx2, fma2(x.p[i], cx2, vv[j].p[i]));
       }
     }
-    if (!active) continue;
 #pragma unroll
     for (int j = 0; j < kVec; ++j)
-      store8<false>(p.dx + static_cast<size_t>(t) * p.lddx, 8 * (static_cast<int>(threadIdx.x) + j * nt), d_, vv[j]);
+      store8<false, kRagged>(p.dx + static_cast<size_t>(t) * p.lddx, col0 + 8 * j * nt, lim, vv[j]);
   }
   grid_launch_dependents();
   if (p.want == 0) return;
   float* part = p.part + static_cast<size_t>(blockIdx.x) * 2 * p.part_d;
-  if (kHold) {
+  if (kNarrow) {
+    // the block's rows share columns: first the rows of a warp, then the warps, in a fixed order
+    float f[2][8];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 v = unpair2(acc[a].p[i]);
+        f[a][2 * i] = v.x;
+        f[a][2 * i + 1] = v.y;
+      }
+#pragma unroll
+    for (int o = 16; o >= 8; o >>= 1) {
+      if (o < span) break;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) f[i >> 3][i & 7] += __shfl_xor_sync(0xffffffffu, f[i >> 3][i & 7], o);
+    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cols = 8 * span, warps = nt >> 5;
+    __syncthreads();  // the ring's memory is used again
+    if (lane < span) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        float4* q = reinterpret_cast<float4*>(dyn + (2 * warp + a) * cols + 8 * lane);
+        q[0] = make_float4(f[a][0], f[a][1], f[a][2], f[a][3]);
+        q[1] = make_float4(f[a][4], f[a][5], f[a][6], f[a][7]);
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * cols; i += nt) {
+      const int a = i >= cols ? 1 : 0, c = i - a * cols;
+      if (c >= p.part_d) continue;
+      float t = 0.f;
+      for (int w = 0; w < warps; ++w) t += dyn[(2 * w + a) * cols + c];
+      part[static_cast<size_t>(a) * p.part_d + c] = t;
+    }
+  } else if (kHold) {
     // rows of part_d floats: 16-byte stores; columns beyond d hold zeros
-    const int c = 8 * threadIdx.x;
 #pragma unroll
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int i = 0; i < 4; i += 2)
-        if (c + 2 * i < p.part_d)
-          *reinterpret_cast<ulonglong2*>(part + static_cast<size_t>(a) * p.part_d + c + 2 * i) = make_ulonglong2(acc[a].p[i], acc[a].p[i + 1]);
+        if (col0 + 2 * i < p.part_d)
+          *reinterpret_cast<ulonglong2*>(part + static_cast<size_t>(a) * p.part_d + col0 + 2 * i) = make_ulonglong2(acc[a].p[i], acc[a].p[i + 1]);
   } else {
     for (int a = 0; a < 2; ++a)
 #pragma unroll
       for (int j = 0; j < kVec; ++j)
         for (int half = 0; half < 2; ++half) {
-          const int c = 8 * (static_cast<int>(threadIdx.x) + j * nt) + 4 * half;
+          const int c = col0 + 8 * j * nt + 4 * half;
           if (c < p.part_d)
             *reinterpret_cast<ulonglong2*>(part + static_cast<size_t>(a) * p.part_d + c) = sums[(2 * (a * kVec + j) + half) * nt + threadIdx.x];
         }

@@ -202,3 +202,59 @@ def test_same_bits_every_time_on_another_stream_and_from_a_graph():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(hg, h) and torch.equal(yg, y) and all(torch.equal(a, b) for a, b in zip(want, gg))
+
+
+# Rows of at most 256 elements share a block (4 or 2 of them a warp up to 64 and 128 elements): numbers of rows around
+# a block's, widths around the limits; wider ones that end inside a vector of eight, in every size of block.
+@pytest.mark.parametrize("T,d", [(1, 64), (31, 64), (33, 8), (70, 63), (129, 65), (4097, 128), (257, 121), (9, 249), (7, 255),
+                                 (40, 729), (301, 1001), (5, 2051), (3, 3333), (4, 4099), (3, 6001), (2, 8190)])
+@pytest.mark.parametrize("sd", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gate,post", [("none", True), ("shared", True), ("token", True)])
+def test_narrow_and_ragged_rows(T, d, sd, gate, post):
+    x, r, how = _case(T, d, sd, torch.float32, gate, post, pad=8 * (T % 2))
+    h, y = B.npd_norm_fwd(x, r, **how)
+    _check_forward(x, r, how, h, y)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    dy, dh = _mat(g, T, d), _mat(g, T, d, sd, pad=16)
+    _check_backward(dy, h, x, dh, how, B.npd_norm_bwd(dy, h, x, dh=dh, **how))
+
+
+@pytest.mark.parametrize("T,d", [(37, 40), (50, 128), (19, 250), (12, 729), (5, 4104)])
+@pytest.mark.parametrize("sd", [torch.bfloat16, torch.float32])
+def test_calls_with_parts_missing_at_every_size_of_block(T, d, sd):
+    for gate in ("none", "shared", "token"):
+        x, r, how = _case(T, d, sd, torch.bfloat16, gate, True)
+        h, y = B.npd_norm_fwd(x, r, **how)
+        g = torch.Generator(device=DEV).manual_seed(3)
+        dy, dh = _mat(g, T, d), _mat(g, T, d, sd)
+        for a, b in ((dy, None), (None, dh)):
+            _check_backward(a, h, x, b, how, B.npd_norm_bwd(a, h, x, dh=b, **how))
+        got = B.npd_norm_bwd(dy, h, x, dh=dh, want_dresidual=False, **how)
+        assert got[1] is None
+        _check_backward(dy, h, x, dh, how, got)
+
+
+def test_rows_that_do_not_exist_add_nothing_without_eps():
+    # a block takes more rows than the call has; their zeros have no finite reciprocal norm when eps is 0
+    for T, d in ((3, 64), (9, 100), (5, 256)):
+        x, r, how = _case(T, d, torch.bfloat16, torch.float32, "shared", True, eps=0.0)
+        h, y = B.npd_norm_fwd(x, r, **how)
+        _check_forward(x, r, how, h, y)
+        g = torch.Generator(device=DEV).manual_seed(4)
+        dy, dh = _mat(g, T, d), _mat(g, T, d)
+        _check_backward(dy, h, x, dh, how, B.npd_norm_bwd(dy, h, x, dh=dh, **how))
+
+
+def test_narrow_rows_behind_the_last_one_and_in_place():
+    x, r, how = _case(21, 72, torch.float32, torch.bfloat16, "token", True)
+    buf = torch.full((32, 72), 7.0, device=DEV)
+    yb = torch.full((32, 72), 7.0, device=DEV, dtype=torch.bfloat16)
+    h, y = B.npd_norm_fwd(x, r, **how)
+    B.npd_norm_fwd(x, r, h=buf[:21], y=yb[:21], **how)
+    assert torch.equal(buf[:21], h) and torch.equal(yb[:21], y) and (buf[21:] == 7).all() and (yb[21:] == 7).all()
+    g = torch.Generator(device=DEV).manual_seed(5)
+    dy, dh = _mat(g, 21, 72), _mat(g, 21, 72, torch.float32)
+    want = B.npd_norm_bwd(dy, h, x, dh=dh, **how)
+    dy1, dh1, gate1 = dy.clone(), dh.clone(), how["gate"].clone()
+    got = B.npd_norm_bwd(dy1, h, x, dh=dh1, dx=dy1, dresidual=dh1, d_gate=gate1, **dict(how, gate=gate1))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
