@@ -92,6 +92,17 @@ LinearPlan linear_plan(const npd_linear_args* a, int sms) {
   return pl;
 }
 
+template <bool kRagged>
+void (*linear_dz_pick(int act))(LinearGradParams) {
+  switch (act) {
+    case NPD_ACT_RELU: return linear_dz_kernel<kActRelu, kRagged>;
+    case NPD_ACT_GELU: return linear_dz_kernel<kActGelu, kRagged>;
+    case NPD_ACT_GELU_TANH: return linear_dz_kernel<kActGeluTanh, kRagged>;
+    case NPD_ACT_SILU: return linear_dz_kernel<kActSilu, kRagged>;
+    default: return linear_dz_kernel<kActNone, kRagged>;
+  }
+}
+
 template <int kG>
 cudaError_t launch_rows(const LinearParams& p, cudaStream_t st) {
   return launch_ex(linear_rows_kernel<kG>, (p.N + 15) / 16, 32 * rows_cfg::kWarps, 0, st, false, p);
@@ -219,11 +230,7 @@ int npd_linear_bwd(const npd_linear_args* a, void* cuda_stream) {
       dz = gp.dz;
       lddz = pl.lddz;
     }
-    auto k = a->activation == NPD_ACT_RELU        ? linear_dz_kernel<kActRelu>
-             : a->activation == NPD_ACT_GELU      ? linear_dz_kernel<kActGelu>
-             : a->activation == NPD_ACT_GELU_TANH ? linear_dz_kernel<kActGeluTanh>
-             : a->activation == NPD_ACT_SILU      ? linear_dz_kernel<kActSilu>
-                                                  : linear_dz_kernel<kActNone>;
+    const auto k = a->N % 8 != 0 ? linear_dz_pick<true>(a->activation) : linear_dz_pick<false>(a->activation);
     cudaError_t e = launch_dim(k, dim3(static_cast<unsigned>((a->N + 255) / 256), static_cast<unsigned>(pl.row_blocks)), 256, 0, st,
                                false, gp);
     ++g_launches;

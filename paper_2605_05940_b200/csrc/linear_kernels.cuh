@@ -322,8 +322,10 @@ struct LinearGradParams {
   float* part;           // [gridDim.y][ldpart] or NULL
 };
 
-template <int kAct>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const LinearGradParams p) {
+// kRagged: N need not be a multiple of 8.  Four blocks of 64 registers per SM: with six of 40 the loop keeps less in
+// flight (M = 8192, N = 16,384 and a dx product of K = 64: GELU 275 us instead of 285, its tanh form 257 instead of 280).
+template <int kAct, bool kRagged>
+__global__ void __launch_bounds__(256, 4) linear_dz_kernel(const LinearGradParams p) {
   __shared__ float sums[8][256 + 8];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = blockIdx.x * 256 + lane * 8;
@@ -334,20 +336,31 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const LinearGradParams p
   for (int i = 0; i < 8; ++i) s.v[i] = 0.f;
   if (c < p.N) {
     // the next row's loads are in flight while this row's slopes are evaluated
+    const int n = p.N - c;
+    const __nv_bfloat16* pd = p.dy + static_cast<size_t>(m0 + warp) * p.lddy + c;
+    const __nv_bfloat16* pz = kAct != kActNone ? p.z + static_cast<size_t>(m0 + warp) * p.ldz + c : nullptr;
+    __nv_bfloat16* po = kAct != kActNone ? p.dz + static_cast<size_t>(m0 + warp) * p.lddz : nullptr;
     Raw8<false> dy = zero8<false>(), zz = zero8<false>();
     auto fetch = [&](int m) {
-      dy = load8<false>(p.dy + static_cast<size_t>(m) * p.lddy, c, p.N);
-      if (kAct != kActNone) zz = load8<false>(p.z + static_cast<size_t>(m) * p.ldz, c, p.N);
+      dy = fetch8<false, kRagged>(pd, 0, n, m == p.M - 1);
+      if (kAct != kActNone) zz = fetch8<false, kRagged>(pz, 0, n, m == p.M - 1);
     };
     if (m0 + warp < m1) fetch(m0 + warp);
     for (int m = m0 + warp; m < m1; m += 8) {
+      if (kRagged && n < 8) {
+        trim8<false>(dy, pd, 0, n, m == p.M - 1);
+        if (kAct != kActNone) trim8<false>(zz, pz, 0, n, m == p.M - 1);
+      }
       V8 g = unpack8<false>(dy);
       const V8 z = unpack8<false>(zz);
+      pd += 8 * p.lddy;
+      if (kAct != kActNone) pz += 8 * p.ldz;
       if (m + 8 < m1) fetch(m + 8);
       if (kAct != kActNone) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g.v[i] *= act_slope(kAct, z.v[i]);
-        store8<false>(p.dz + static_cast<size_t>(m) * p.lddz, c, p.N, g);
+        store8<false, kRagged>(po, c, p.N, g);
+        po += 8 * p.lddz;
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) s.v[i] += g.v[i];
