@@ -203,8 +203,9 @@ NormKernel norm_bwd_pick(const NormPlan& pl) {
 }
 template <bool kF32>
 NormKernel norm_bwd_pick(const NormPlan& pl, int form, bool token_gate) {
-  if (pl.vec == 2) return norm_bwd_kernel<kF32, 2, 0, false, 512, false>;
-  if (pl.vec == 4) return norm_bwd_kernel<kF32, 4, 0, false, 512, false>;
+  if (pl.vec > 1 && form < 2) return pl.vec == 2 ? norm_bwd_kernel<kF32, 2, 0, false, 512, false> : norm_bwd_kernel<kF32, 4, 0, false, 512, false>;
+  if (pl.vec == 2) return token_gate ? norm_bwd_kernel<kF32, 2, 2, true, 512, false> : norm_bwd_kernel<kF32, 2, 2, false, 512, false>;
+  if (pl.vec == 4) return token_gate ? norm_bwd_kernel<kF32, 4, 2, true, 512, false> : norm_bwd_kernel<kF32, 4, 2, false, 512, false>;
   if (form == 0) return norm_bwd_pick<kF32, 0, false>(pl);
   if (token_gate) return form == 1 ? norm_bwd_pick<kF32, 1, true>(pl) : norm_bwd_pick<kF32, 2, true>(pl);
   return form == 1 ? norm_bwd_pick<kF32, 1, false>(pl) : form == 2 ? norm_bwd_pick<kF32, 2, false>(pl) : norm_bwd_pick<kF32, 3, false>(pl);
@@ -259,11 +260,11 @@ int npd_norm_bwd(const npd_norm_args* a, void* cuda_stream) {
   const bool sf = a->stream_dtype == NPD_DTYPE_F32;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool token_gate = p.gate != nullptr && p.ldg != 0;
-  const bool full = pl.vec == 1 && p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr && p.dres != nullptr &&
+  const bool full = p.dy != nullptr && p.dh != nullptr && p.x != nullptr && p.dx != nullptr && p.dres != nullptr &&
                     (!token_gate || p.dgate != nullptr);
   const int form = !full ? 0 : a->d % 8 != 0 ? 1 : a->d % 256 != 0 || token_gate ? 2 : 3;
   const NormKernel k = sf ? norm_bwd_pick<true>(pl, form, token_gate) : norm_bwd_pick<false>(pl, form, token_gate);
-  const int ring = full && !sf ? norm_cfg::kRing * pl.threads * 16 * (token_gate ? 5 : 4) : 0;
+  const int ring = pl.vec == 1 && full && !sf ? norm_cfg::kRing * pl.threads * 16 * (token_gate ? 5 : 4) : 0;
   const int smem = std::max(ring, pl.smem);
   if (smem > 0 && set_smem(k, norm_cfg::kMaxSmem) != NPD_OK) return NPD_ECUDA;
   cudaError_t e = launch_ex(k, pl.grid, pl.threads, smem, st, false, p);

@@ -509,7 +509,8 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
 // that they wait for).  kVec == 4: only the sums fit, gains are re-read.
 // kForm > 0: every operand and result exists, and with kGate every token has its own gate (without it none has).  2: d
 // is a multiple of 8 besides (no vector is partly outside the row); 3: of 256 (no thread is; d = 2048, T = 40,000: 160 us,
-// as form 2 172 us, as form 1 170; an fp32 stream as form 1 296 us instead of 228).  A call with a missing part takes
+// as form 2 172 us, as form 1 170; an fp32 stream as form 1 296 us instead of 228).  kVec > 1: 2 or 0 (d = 8192, T =
+// 10,000: 234 us as form 2, 254 as form 0; d = 12,288, T = 6664: 434 and 572 us).  A call with a missing part takes
 // form 0, which tests for it (a per-token gate at d = 1536, T = 53,328: 372 us in form 0, 202 us in its own).
 // kNarrow: see norm_cfg (d = 128, T = 65,536, bf16: 23 us; a block of one warp per row took 41 us).
 template <bool kF32, int kVec, int kForm, bool kGate, int kThreads, bool kNarrow>
@@ -518,10 +519,10 @@ __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_kernel(cons
   __shared__ SumBuf<1> red1[2];
   extern __shared__ __align__(16) float dyn[];  // sums over rows, or the ring
   constexpr bool kHold = kVec == 1, kFull = kForm > 0, kRagged = kForm < 2;
-  constexpr bool kRows = kFull && !kF32;  // rows arrive through the ring
+  constexpr bool kRows = kHold && kFull && !kF32;  // rows arrive through the ring
   constexpr bool kKept = kVec == 2;       // gains kept in shared memory
   constexpr int kRing = norm_cfg::kRing;
-  constexpr bool kNext = kFull && kF32 && !kRagged;  // the next row is in flight in registers
+  constexpr bool kNext = kHold && kFull && kF32 && !kRagged;  // the next row is in flight in registers
   constexpr size_t es = kF32 ? 4 : 2;
   const int nt = blockDim.x;
   const int span = kNarrow ? p.span : nt, sub = kNarrow ? static_cast<int>(threadIdx.x) / span : 0, rows = kNarrow ? nt / span : 1;
