@@ -430,7 +430,8 @@ def _scope(dev, stream):
     if stream is None:
         return _no_scope if dev == torch.cuda.current_device() else torch.cuda.device(dev)
     if not hasattr(stream, "cuda_stream"):
-        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+        # handle 0 is the default stream; ExternalStream(0) would be another one, out of torch's pool
+        stream = torch.cuda.ExternalStream(int(stream), device=dev) if int(stream) else torch.cuda.default_stream(dev)
     if stream.device.index != dev:
         raise NpdError(NPD_EINVAL, "stream of another device")
     return torch.cuda.stream(stream)
