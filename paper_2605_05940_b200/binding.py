@@ -448,6 +448,14 @@ def _workspace(nbytes, device):
     return t, (t.data_ptr() + 1023) & ~1023
 
 
+def _given_workspace(t, where, dev):
+    """Address and size in bytes of a caller's workspace: dense memory on GPU `dev`.  The library checks its size and
+    alignment, but takes the address on trust."""
+    if t.get_device() != dev or not t.is_contiguous():
+        raise NpdError(NPD_EWORKSPACE, where)
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _norm_args(where, dev, shape, x, gate, post_weight, pre_weight, post_norm, eps, weight_offset, residual_scale,
                branch_scale, stream_dtype):
     T, d = shape
@@ -560,7 +568,7 @@ def npd_norm_bwd(dy, h, x=None, *, dh=None, gate=None, post_weight=None, pre_wei
                 workspace, a.workspace = _workspace(n.value, device)
                 a.workspace_bytes = n.value
             else:
-                a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+                a.workspace, a.workspace_bytes = _given_workspace(workspace, where, dev)
         _check(lib().npd_norm_bwd(a, _current(dev)), where)
     return dx, dresidual, d_post, d_pre, d_gate
 
@@ -644,7 +652,7 @@ def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_
             workspace, a.workspace = _workspace(n.value, device)
             a.workspace_bytes = n.value
         else:
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            a.workspace, a.workspace_bytes = _given_workspace(workspace, where, dev)
         _check(lib().npd_linear_bwd(a, _current(dev)), where)
     return dx, dw, dbias
 
@@ -749,8 +757,8 @@ class CEStep:
                 self._workspace, a.workspace = _workspace(n.value, device)
                 a.workspace_bytes = n.value
             else:
-                self._workspace, a.workspace = workspace, workspace.data_ptr()
-                a.workspace_bytes = workspace.numel() * workspace.element_size()
+                self._workspace = workspace
+                a.workspace, a.workspace_bytes = _given_workspace(workspace, where, dev)
 
     def run(self, stream=None):
         """Enqueues the step on `stream` (default: the current one of the tensors' GPU)."""

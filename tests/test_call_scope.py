@@ -1,5 +1,7 @@
-"""What a call does with the `stream` it is given (binding._scope).  The first tests need no GPU: torch's stream
-objects are replaced."""
+"""What a call does with the `stream` and the `workspace` it is given.  The tests that are not marked need no GPU:
+torch's stream objects, or the library behind the binding, are replaced."""
+
+import contextlib
 
 import types
 
@@ -49,3 +51,56 @@ def test_calls_on_handle_zero_follow_the_default_stream():
            B.npd_cross_entropy(x, w, labels, stream=0)[0])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+class _Elsewhere(torch.Tensor):
+    """A tensor that says it lies on another GPU."""
+    def get_device(self):
+        return 1
+
+
+def _calls_with(workspace):
+    """The calls that take a workspace, on CPU tensors."""
+    bf16 = torch.bfloat16
+    x, w = torch.zeros((8, 64), dtype=bf16), torch.zeros((16, 64), dtype=bf16)
+    return {
+        "norm": lambda: B.npd_norm_bwd(x, x, x, pre_weight=torch.ones(64), workspace=workspace),
+        "linear": lambda: B.npd_linear_bwd(torch.zeros((8, 16), dtype=bf16), x, w, workspace=workspace),
+        "ce": lambda: B.CEStep(x, w, torch.zeros(8, dtype=torch.int32), workspace=workspace).run(),
+    }
+
+
+@pytest.mark.parametrize("op", ["norm", "linear", "ce"])
+@pytest.mark.parametrize("kind", ["dense", "elsewhere", "strided"])
+def test_a_workspace_elsewhere_or_with_gaps_is_refused(monkeypatch, op, kind):
+    # the address would go to the kernels as it is
+    launched = []
+    done = lambda args, stream: launched.append(args.workspace) or B.NPD_OK
+    monkeypatch.setattr(B, "lib", lambda: types.SimpleNamespace(npd_norm_bwd=done, npd_linear_bwd=done, npd_ce_fwd_bwd=done,
+                                                                npd_strerror=lambda code: b""))
+    monkeypatch.setattr(B, "_device_of", lambda t, where: t.get_device())
+    monkeypatch.setattr(B, "_scope", lambda dev, stream: contextlib.nullcontext())
+    monkeypatch.setattr(B, "_current", lambda dev: 0)
+    room = torch.zeros(1 << 16, dtype=torch.uint8)
+    ws = {"dense": room, "elsewhere": room.as_subclass(_Elsewhere), "strided": room[::2]}[kind]
+    call = _calls_with(ws)[op]
+    if kind == "dense":
+        call()
+        assert launched == [room.data_ptr()]
+        return
+    with pytest.raises(B.NpdError) as e:
+        call()
+    assert e.value.code == B.NPD_EWORKSPACE and not launched
+
+
+@pytest.mark.gpu
+def test_a_workspace_in_host_memory_is_refused():
+    bf16 = torch.bfloat16
+    x, w = torch.zeros((8, 64), dtype=bf16, device="cuda"), torch.zeros((16, 64), dtype=bf16, device="cuda")
+    host = torch.zeros(1 << 24, dtype=torch.uint8)
+    for call in (lambda: B.npd_norm_bwd(x, x, x, pre_weight=torch.ones(64, device="cuda"), workspace=host),
+                 lambda: B.npd_linear_bwd(torch.zeros((8, 16), dtype=bf16, device="cuda"), x, w, workspace=host),
+                 lambda: B.CEStep(x, w, torch.zeros(8, dtype=torch.int32, device="cuda"), workspace=host)):
+        with pytest.raises(B.NpdError) as e:
+            call()
+        assert e.value.code == B.NPD_EWORKSPACE
