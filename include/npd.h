@@ -437,8 +437,8 @@ enum {
  * Either gradient may be NULL (a frozen head, for instance); the work for it is then left out.
  *
  * Layouts and alignment as in npd_kd_args: row-major, row strides in ELEMENTS, the four matrices 16-byte
- * aligned with row strides that are multiples of 16 bytes, d a multiple of 64, any T >= 1, V >= 1 with T V <= 2^46.  Outputs may not
- * overlap inputs or each other (NPD_EINVAL).
+ * aligned with row strides that are multiples of 16 bytes, d a multiple of 64.  Limits (NPD_ESHAPE): 1 <= T, V <= 2^30,
+ * d <= 2^26, and T V, T d and V d <= 2^46.  Outputs may not overlap inputs or each other (NPD_EINVAL).
  *
  * nll, lse and d_weight are bitwise reproducible; d_hidden is summed over pieces of the vocabulary with
  * fp32 atomic adds whose order is not fixed (a few of its bf16 elements may round differently).  The logit

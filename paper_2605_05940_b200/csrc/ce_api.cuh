@@ -64,9 +64,11 @@ int check_ce(const npd_ce_args* a, bool need_pointers) {
   if (a->d_weight_dtype != NPD_DTYPE_BF16 && a->d_weight_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
   if ((a->flags & ~(NPD_CE_ACCUMULATE_DW | NPD_CE_SERIALIZE_LAUNCHES)) || a->grad_chunk_cols < 0) return NPD_EINVAL;
   if ((a->flags & NPD_CE_ACCUMULATE_DW) && a->d_weight_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
-  // row numbers and 256-wide tiles are 32-bit
-  if (a->T > (1 << 30) || a->V > (1 << 30)) return NPD_ESHAPE;
-  if ((a->T / 256 + 1ll) * (a->V / 256 + 1ll) > (1 << 30)) return NPD_ESHAPE;
+  // Row numbers, columns, numbers of tiles and the bytes of eight tokens (ce_rows_kernel) are 32-bit.  A product of
+  // 2^46 is at most 2^30 + (2^30 + 2^30) / 256 + 1 tiles of 256 x 256.
+  if (a->T > (1 << 30) || a->V > (1 << 30) || a->d > (1 << 26)) return NPD_ESHAPE;
+  const long long nt = a->T, nv = a->V, nd = a->d;
+  if (std::max({nt * nv, nt * nd, nv * nd}) > 1ll << 46) return NPD_ESHAPE;
   if (a->d % 64 != 0) return NPD_ESHAPE;
   if (!need_pointers) return NPD_OK;
   if (a->hidden == nullptr || a->weight == nullptr || a->labels == nullptr || a->nll == nullptr) return NPD_EINVAL;

@@ -79,3 +79,27 @@ def test_struct_layout_matches_the_header(tmp_path):
     subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(c), "-o", str(tmp_path / "t")], check=True)
     got = [int(v) for v in subprocess.run([str(tmp_path / "t")], capture_output=True, text=True, check=True).stdout.split()]
     assert got == [C.sizeof(B.npd_ce_args)] + [getattr(B.npd_ce_args, f).offset for f in fields]
+
+
+def _wide(d, **kw):
+    return dict(dict(d=d, ldh=d, ldw=d, ld_dh=d, ld_dw=d), **kw)
+
+
+@pytest.mark.parametrize("kw", [
+    # from d = 2^27 on the bytes of eight tokens pass 32 bits; at 2^28 they would wrap to none at all
+    _wide(1 << 27), _wide(1 << 28), _wide((1 << 28) + 64, T=1, V=2, d_hidden=None, d_weight=None), _wide(1 << 30),
+    _wide((1 << 26) + 64), _wide(1 << 26, V=(1 << 20) + 1), _wide(1 << 26, T=(1 << 20) + 1),
+    dict(T=(1 << 23) + 1, V=1 << 23), dict(T=1 << 30, V=(1 << 16) + 1),
+])
+def test_extents_beyond_the_limits_are_refused(kw):
+    assert _run(**kw) == B.NPD_ESHAPE
+    n = C.c_size_t(0)
+    assert B.lib().npd_ce_workspace_bytes(C.byref(_args(**kw)), C.byref(n)) == B.NPD_ESHAPE
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up")
+@pytest.mark.parametrize("kw", [dict(T=1 << 23, V=1 << 23), dict(T=1 << 30, V=1 << 16), dict(T=(1 << 23) - 1, V=(1 << 23) + 1),
+                                _wide(1 << 26)])
+def test_extents_up_to_the_limits_pass(kw):
+    n = C.c_size_t(0)
+    assert B.lib().npd_ce_workspace_bytes(C.byref(_args(**kw)), C.byref(n)) == B.NPD_ECUDA
