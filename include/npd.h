@@ -502,8 +502,9 @@ enum { NPD_LINEAR_ACCUMULATE_DW = 1 /* add into dw instead of overwriting it (f3
  * and dw (dbias sums the unrounded values), so an fp32 dw has fp32 sums of bf16-rounded terms.
  *
  * Row-major, row strides in ELEMENTS, matrices on 16-byte boundaries with row strides that are multiples of 16
- * bytes; any M, N, K >= 1 with M N, M K and N K <= 2^46.  bias needs no alignment beyond its type's.  y may be residual itself (same pointer and
- * stride); any other overlap of a result with an operand or another result is refused (NPD_EINVAL).
+ * bytes.  Limits (NPD_ESHAPE): 1 <= M, N, K <= 2^30, and M N, M K and N K <= 2^46.  bias needs no alignment beyond
+ * its type's.  y may be residual itself (same pointer and stride); any other overlap of a result with an operand or
+ * another result is refused (NPD_EINVAL).
  *
  * Every result is bitwise reproducible, but for a dw that is added to (atomic adds, one per element and call).
  * `status` (int32[1], may be NULL) receives NPD_ETIMEOUT if a bounded wait ran out in the forward, else it is left

@@ -14,12 +14,11 @@ int check_linear(const npd_linear_args* a, bool backward, bool need_pointers) {
   if (a->dw_dtype != NPD_DTYPE_BF16 && a->dw_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
   if (a->flags & ~NPD_LINEAR_ACCUMULATE_DW) return NPD_EINVAL;
   if ((a->flags & NPD_LINEAR_ACCUMULATE_DW) && a->dw_dtype != NPD_DTYPE_F32) return NPD_EINVAL;
-  // extents and numbers of tiles are 32-bit
+  // extents and numbers of tiles are 32-bit: a product of 2^46 is at most 2^30 + (2^30 + 2^30) / 256 + 1 tiles
   if (a->M > (1 << 30) || a->N > (1 << 30) || a->K > (1 << 30)) return NPD_ESHAPE;
-  auto tiles = [](long long r, long long c) { return ((r + 255) / 256) * ((c + 255) / 256); };
-  if (std::max({tiles(a->M, a->N), tiles(a->M, a->K), tiles(a->N, a->K)}) > (1 << 30)) return NPD_ESHAPE;
-  if (!need_pointers) return NPD_OK;
   const long long M = a->M, N = a->N, K = a->K;
+  if (std::max({M * N, M * K, N * K}) > 1ll << 46) return NPD_ESHAPE;
+  if (!need_pointers) return NPD_OK;
   const long long ye = a->y_dtype == NPD_DTYPE_F32 ? 4 : 2, we = a->dw_dtype == NPD_DTYPE_F32 ? 4 : 2,
                   be = a->bias_dtype == NPD_DTYPE_F32 ? 4 : 2;
   struct M_ { const void* p; int64_t ld; long long cols, es; };

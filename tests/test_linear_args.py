@@ -102,3 +102,15 @@ def test_struct_layout_matches_the_header(tmp_path):
     subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(c), "-o", str(tmp_path / "t")], check=True)
     got = [int(v) for v in subprocess.run([str(tmp_path / "t")], capture_output=True, text=True, check=True).stdout.split()]
     assert got == [C.sizeof(B.npd_linear_args)] + [getattr(B.npd_linear_args, f).offset for f in fields]
+
+
+@pytest.mark.parametrize("kw", [dict(M=(1 << 23) + 1, N=1 << 23), dict(N=1 << 30, K=(1 << 16) + 1), dict(M=1 << 30, K=(1 << 16) + 1)])
+def test_products_beyond_the_limit_are_refused(kw):
+    assert B.lib().npd_linear_workspace_bytes(_args(**kw), C.byref(C.c_size_t(0))) == B.NPD_ESHAPE
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are made up")
+@pytest.mark.parametrize("kw", [dict(M=1 << 23, N=1 << 23), dict(M=(1 << 23) + 1, N=(1 << 23) - 1), dict(N=1 << 30, K=1 << 16)])
+def test_products_up_to_the_limit_pass(kw):
+    # whole tiles beyond a border do not count against it
+    assert B.lib().npd_linear_workspace_bytes(_args(**kw), C.byref(C.c_size_t(0))) == B.NPD_ECUDA
