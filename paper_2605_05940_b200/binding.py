@@ -662,7 +662,8 @@ class NormJoin:
     branch_scale * gate * (norm of x, or x), hidden states = norm of h (npd_norm_fwd / npd_norm_bwd), with its
     buffers.  Given to KDStep or CEStep as `norm`, every run of the step first writes the step's hidden states and
     afterwards turns their gradient into those of x, residual, gate and gains: dx, dresidual, d_post_weight,
-    d_pre_weight, d_gate.  Arguments as for npd_norm_fwd."""
+    d_pre_weight, d_gate.  For a step without d_hidden (scoring, a head trained alone) the join is made with
+    grads=False; otherwise the step refuses it.  Arguments as for npd_norm_fwd."""
 
     def __init__(self, x, residual=None, *, grads=True, **how):
         self.x, self.residual, self.how, self.grads = x, residual, how, grads
@@ -693,6 +694,12 @@ class NormJoin:
             n = C.c_size_t(0)
             _check(lib().npd_norm_workspace_bytes(a, n), "npd_norm_workspace_bytes")
             self._workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
+
+    def attach(self, d_hidden):
+        """What a step checks when it is made.  Gradients that no run would write are refused: their buffers would pass
+        for results."""
+        if self.grads and d_hidden is None:
+            raise NpdError(NPD_EINVAL, "NormJoin: gradients of a step without d_hidden")
 
     def forward(self, hidden, stream=None):
         npd_norm_fwd(self.x, self.residual, h=self.h, y=hidden, stream=stream, **self.how)
@@ -744,6 +751,8 @@ class CEStep:
                 if accumulate_dw:
                     d_weight.zero_()
             self.d_hidden, self.d_weight = d_hidden, d_weight
+            if norm is not None:
+                norm.attach(d_hidden)
             if d_hidden is not None:
                 a.ld_dh, a.d_hidden = _matrix(d_hidden, where, dev, shape, bf16), d_hidden.data_ptr()
             if d_weight is not None:
@@ -766,7 +775,7 @@ class CEStep:
             self.norm.forward(self._inputs[0], stream)
         with _scope(self._dev, stream):
             _check(lib().npd_ce_fwd_bwd(self.args, _current(self._dev)), "npd_ce_fwd_bwd")
-        if self.norm is not None and self.d_hidden is not None and self.norm.grads:
+        if self.norm is not None and self.norm.grads:
             self.norm.backward(self.d_hidden, stream)
 
     def status(self, stream=None) -> int:
@@ -807,6 +816,8 @@ class KDStep:
                                              device=dev) if grads else None)
         self.d_weight = (torch.empty_strided((V, d), (batch.weight.stride(0), 1), dtype=dw_dtype,
                                              device=dev) if grads else None)
+        if norm is not None:
+            norm.attach(self.d_hidden)
         self.grad_scale = (1.0 / max(batch.n_loss, 1)) if grad_scale is None else grad_scale
         self._kw = dict(cu_seqlens=batch.cu_seqlens, loss_mask=batch.loss_mask, labels=batch.labels,
                         temperature=batch.tau, grad_scale=self.grad_scale, kl=self.kl,
@@ -830,7 +841,7 @@ class KDStep:
         if self.norm is not None:
             self.norm.forward(self.batch.hidden, stream)
         npd_kd_fwd_bwd(args, stream)
-        if self.norm is not None and self.d_hidden is not None and self.norm.grads:
+        if self.norm is not None and self.norm.grads:
             self.norm.backward(self.d_hidden, stream)
 
     def phase_names(self):
