@@ -406,6 +406,23 @@ def _vector(t, where, dev, n, dtype):
     return t.data_ptr()
 
 
+def _touch(a, b):
+    """Whether two tensors share a byte.  Column windows of one wider buffer may lie between each other's rows."""
+    if a is None or b is None or a.get_device() != b.get_device():
+        return False
+    span = lambda t: (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))) * t.element_size()
+    a0, b0 = a.data_ptr(), b.data_ptr()
+    if a0 + span(a) <= b0 or b0 + span(b) <= a0:
+        return False
+    if a.dim() != 2 or b.dim() != 2:
+        return True
+    pitch, wa, wb = (v * t.element_size() for t, v in ((a, a.stride(0)), (a, a.shape[1]), (b, b.shape[1])))
+    if pitch != b.stride(0) * b.element_size() or max(wa, wb) > pitch:
+        return True
+    delta = (b0 - a0) % pitch
+    return delta < wa or pitch - delta < wb
+
+
 def _new(shape, dtype, device):
     """An uninitialised matrix whose rows start on 16-byte boundaries."""
     cols = shape[1]
@@ -663,7 +680,8 @@ class NormJoin:
     buffers.  Given to KDStep or CEStep as `norm`, every run of the step first writes the step's hidden states and
     afterwards turns their gradient into those of x, residual, gate and gains: dx, dresidual, d_post_weight,
     d_pre_weight, d_gate.  For a step without d_hidden (scoring, a head trained alone) the join is made with
-    grads=False; otherwise the step refuses it.  Arguments as for npd_norm_fwd."""
+    grads=False; otherwise the step refuses it.  The backward reads x, gate and gains again, so the step's hidden
+    states and d_hidden lie apart from them (hidden may be x's memory with grads=False).  Arguments as for npd_norm_fwd."""
 
     def __init__(self, x, residual=None, *, grads=True, **how):
         self.x, self.residual, self.how, self.grads = x, residual, how, grads
@@ -695,11 +713,16 @@ class NormJoin:
             _check(lib().npd_norm_workspace_bytes(a, n), "npd_norm_workspace_bytes")
             self._workspace = torch.empty(n.value, dtype=torch.uint8, device=device)
 
-    def attach(self, d_hidden):
-        """What a step checks when it is made.  Gradients that no run would write are refused: their buffers would pass
-        for results."""
-        if self.grads and d_hidden is None:
+    def attach(self, hidden, d_hidden):
+        """What a step checks when it is made.  Gradients that no run would write are refused (their buffers would pass
+        for results), and so are steps that write over what the backward reads after them."""
+        if not self.grads:
+            return
+        if d_hidden is None:
             raise NpdError(NPD_EINVAL, "NormJoin: gradients of a step without d_hidden")
+        for t in (self.x, *(self.how.get(k) for k in ("gate", "post_weight", "pre_weight"))):
+            if _touch(hidden, t) or _touch(d_hidden, t):
+                raise NpdError(NPD_EINVAL, "NormJoin: the step writes over an operand of the join")
 
     def forward(self, hidden, stream=None):
         npd_norm_fwd(self.x, self.residual, h=self.h, y=hidden, stream=stream, **self.how)
@@ -752,7 +775,7 @@ class CEStep:
                     d_weight.zero_()
             self.d_hidden, self.d_weight = d_hidden, d_weight
             if norm is not None:
-                norm.attach(d_hidden)
+                norm.attach(hidden, d_hidden)
             if d_hidden is not None:
                 a.ld_dh, a.d_hidden = _matrix(d_hidden, where, dev, shape, bf16), d_hidden.data_ptr()
             if d_weight is not None:
@@ -817,7 +840,7 @@ class KDStep:
         self.d_weight = (torch.empty_strided((V, d), (batch.weight.stride(0), 1), dtype=dw_dtype,
                                              device=dev) if grads else None)
         if norm is not None:
-            norm.attach(self.d_hidden)
+            norm.attach(batch.hidden, self.d_hidden)
         self.grad_scale = (1.0 / max(batch.n_loss, 1)) if grad_scale is None else grad_scale
         self._kw = dict(cu_seqlens=batch.cu_seqlens, loss_mask=batch.loss_mask, labels=batch.labels,
                         temperature=batch.tau, grad_scale=self.grad_scale, kl=self.kl,

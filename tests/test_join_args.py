@@ -64,3 +64,34 @@ def test_gradients_that_no_run_would_write_are_refused(calls, kind):
     del calls[:]
     step.run()
     assert calls[0] == "npd_norm_fwd" and "npd_norm_bwd" not in calls
+
+
+@pytest.mark.parametrize("kind", ["ce", "kd"])
+def test_hidden_states_over_the_branch_are_refused(calls, kind):
+    # the forward could write y over x, but the backward would then read y as x
+    x = _mat()
+    with pytest.raises(B.NpdError) as e:
+        _step(kind, x, True, B.NormJoin(x, _mat(), pre_weight=torch.ones(D)))
+    assert e.value.code == B.NPD_EINVAL
+    _step(kind, x, False, B.NormJoin(x, _mat(), pre_weight=torch.ones(D), grads=False)).run()
+    both = _mat(T, 2 * D + 16)             # windows of one buffer, side by side, are apart
+    _step(kind, both[:, :D], True, B.NormJoin(both[:, D + 8:2 * D + 8], _mat())).run()
+    with pytest.raises(B.NpdError):
+        _step(kind, both[:, :D], True, B.NormJoin(both[:, D - 8:2 * D - 8], _mat()))
+
+
+def test_d_hidden_over_an_operand_of_the_join_is_refused(calls):
+    x, gate = _mat(), torch.zeros((T, D), dtype=BF16)
+    for other in (x, gate):
+        with pytest.raises(B.NpdError) as e:
+            _step("ce", _mat(), True, B.NormJoin(x, _mat(), gate=gate), d_hidden=other)
+        assert e.value.code == B.NPD_EINVAL
+    _step("ce", _mat(), True, B.NormJoin(x, _mat(), gate=gate), d_hidden=_mat()).run()
+
+
+def test_touch_knows_the_rows_of_a_window():
+    base = torch.zeros((8, 32))
+    assert B._touch(base, base) and B._touch(base, base[3:4]) and not B._touch(base[:4], base[4:])
+    assert not B._touch(base[:, :8], base[:, 8:16]) and not B._touch(base[:, 16:], base[1:, :16])
+    assert B._touch(base[:, :9], base[:, 8:16]) and B._touch(base[:, 16:], base[:, 15:17])
+    assert not B._touch(base, torch.zeros((8, 32))) and not B._touch(base, None) and B._touch(base[0], base[:1])
