@@ -41,12 +41,13 @@
  *     (a cudaStream_t passed as void*; NULL = the legacy default stream).
  *     Results are ready when the stream has been synchronised.  The exceptions are spelled out
  *     where they are declared: npd_kd_forward_noalloc works in a fixed array inside the library
- *     image, and two per-thread diagnostic counters (npd_last_launch_count,
- *     npd_last_copy_bytes) remember the last call for benchmarks.
+ *     image, npd_device_status reads a word per device, and two per-thread diagnostic counters
+ *     (npd_last_launch_count, npd_last_copy_bytes) remember the last call for benchmarks.
  *   - Return value: NPD_OK (0) or a negative npd_status.  Argument errors are
  *     found on the host before anything is launched.  Errors found on the device
  *     (malformed cu_seqlens, a bounded wait that ran out) are recorded in the
- *     workspace and read with npd_last_status().
+ *     workspace and read with npd_last_status(); a wait that ran out is also recorded
+ *     per device and read with npd_device_status().
  *   - No exceptions, no abort(), no device traps.  Every device-side wait on an mbarrier is
  *     bounded (about 2 s of SM clocks).  When one runs out the CTA raises an abort flag that all
  *     its roles poll; warps that meet at named barriers decide together, through a vote at
@@ -316,7 +317,8 @@ int npd_perplexity(int32_t N, const int32_t* seg, const float* nll_s_sum, const 
  * tensor kernels would otherwise never run on a healthy device).  Launches one small CTA that
  * waits, with the same bounded wait and the same group vote the tensor kernels use, on a barrier
  * nothing arrives on, for `limit_cycles` SM clock cycles (1 .. 1e8; a millisecond is about 2e6).
- * out3 (DEVICE, int32[3], cleared by the call): [0] the status word, NPD_ETIMEOUT afterwards;
+ * out3 (DEVICE, int32[3], cleared by the call): [0] the status word, NPD_ETIMEOUT afterwards (in
+ * npd_device_status too);
  * [1] 1 if every thread's wait gave up; [2] cycles thread 0 spent waiting.  No copy or MMA is in
  * flight in that kernel and it always terminates.
  */
@@ -340,6 +342,14 @@ int npd_debug_chunk_schedule(int32_t row_blocks, int32_t d, int32_t chunk_cols, 
  * workspace that npd_kd_fwd_bwd used into *host_status (HOST): NPD_OK,
  * NPD_ESEQ, NPD_ETIMEOUT or (debug checks) NPD_EDATA.  Returns NPD_ECUDA if the stream itself failed. */
 int npd_last_status(const void* workspace, void* cuda_stream, int32_t* host_status);
+
+/* Synchronises `cuda_stream`, then reads the current device's own status word into *host_status (HOST) and clears
+ * it: NPD_ETIMEOUT if a bounded wait of any kernel of the library on this device has run out since the word was
+ * last read, else NPD_OK.  It answers for the calls whose status word the caller does not hold - npd_gemm_bf16,
+ * npd_linear_fwd with status NULL, a workspace that has been given back - and does not say which of them it was:
+ * after NPD_ETIMEOUT take the results of all calls since the last reading as undefined.  Calls still running on other
+ * streams may set the word after it was read.  Not for use inside a stream capture. */
+int npd_device_status(void* cuda_stream, int32_t* host_status);
 
 /* HOST.  Static description of a status code. */
 const char* npd_strerror(int status);

@@ -40,7 +40,8 @@ EXPORTS = ("npd_workspace_bytes", "npd_phase_count", "npd_kd_fwd_bwd", "npd_kd_f
            "npd_kd_forward_noalloc", "npd_pack_sequences", "npd_last_copy_bytes",
            "npd_kd_fwd_bwd_host_streams", "npd_perplexity", "npd_selftest_wait_timeout",
            "npd_debug_chunk_schedule", "npd_norm_fwd", "npd_norm_bwd", "npd_norm_workspace_bytes",
-           "npd_ce_fwd_bwd", "npd_ce_workspace_bytes", "npd_linear_fwd", "npd_linear_bwd", "npd_linear_workspace_bytes")
+           "npd_ce_fwd_bwd", "npd_ce_workspace_bytes", "npd_linear_fwd", "npd_linear_bwd", "npd_linear_workspace_bytes",
+           "npd_device_status")
 NPD_STATIC_SCRATCH_BYTES = 48 * 1024 * 1024
 
 
@@ -137,6 +138,7 @@ def lib() -> C.CDLL:
         l.npd_select.argtypes = ([C.c_int32] + [C.c_void_p] * 5 + [C.c_int32, C.c_float, C.c_float, C.c_int32]
                                  + [C.c_void_p] * 6)
         l.npd_last_status.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(C.c_int32)]
+        l.npd_device_status.argtypes = [C.c_void_p, C.POINTER(C.c_int32)]
         l.npd_last_launch_count.argtypes = []
         l.npd_last_copy_bytes.argtypes = [C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         l.npd_kd_forward_noalloc.argtypes = [C.POINTER(npd_kd_args), C.c_void_p, C.POINTER(C.c_int32)]
@@ -253,6 +255,19 @@ def npd_kd_forward_noalloc(args: npd_kd_args, stream=None, want_status: bool = F
 def npd_last_status(workspace: torch.Tensor, stream=None) -> int:
     out = C.c_int32(0)
     _check(lib().npd_last_status(workspace.data_ptr(), _stream(stream), C.byref(out)), "npd_last_status")
+    return out.value
+
+
+def npd_device_status(device=None, stream=None) -> int:
+    """Waits for `stream` (default: the current one) and returns NPD_ETIMEOUT if a bounded wait of any kernel of the
+    library on this GPU (default: the current one) has run out since the last time this was asked, else NPD_OK.  For the
+    calls that keep no status word for their caller: npd_gemm_bf16, npd_linear_fwd and npd_linear_bwd, npd_cross_entropy."""
+    out = C.c_int32(0)
+    index = device if isinstance(device, int) else None if device is None else torch.device(device).index
+    if index is None:
+        index = torch.cuda.current_device()
+    with _scope(index, stream):
+        _check(lib().npd_device_status(_current(index), C.byref(out)), "npd_device_status")
     return out.value
 
 
@@ -594,7 +609,8 @@ def npd_linear_fwd(x, weight, *, bias=None, activation=NPD_ACT_NONE, residual=No
                    y_dtype=torch.bfloat16, y=None, preact=None, status=None, stream=None):
     """y = act(x weight^T + bias) + residual (see npd_linear_args in include/npd.h).  x bf16 [M, K], weight bf16
     [N, K], bias bf16 or f32 [N], residual of y's type [M, N].  Results go to y and preact or to new tensors
-    (want_preact: the bf16 pre-activation that the backward needs); returns (y, preact)."""
+    (want_preact: the bf16 pre-activation that the backward needs); returns (y, preact).  A wait that ran out on the
+    device shows in `status`, int32[1], and in npd_device_status."""
     where = "npd_linear_fwd"
     dev = _device_of(x, where)
     if x.dim() != 2 or weight.dim() != 2:
@@ -632,7 +648,8 @@ def npd_linear_bwd(dy, x, weight, *, preact=None, activation=NPD_ACT_NONE, want_
                    dw_dtype=torch.bfloat16, dx=None, dw=None, accumulate_dw=False, workspace=None, stream=None):
     """Gradients of npd_linear_fwd from dy bf16 [M, N]: (dx bf16 [M, K], dw [N, K], dbias f32 [N]), None for what
     is not wanted.  preact is the forward's (not needed without an activation), x only for dw.  An f32 dw with
-    accumulate_dw is added to (a new one starts at zero).  The gradient of the residual is dy itself."""
+    accumulate_dw is added to (a new one starts at zero).  The gradient of the residual is dy itself.  A wait that ran
+    out on the device shows in npd_device_status, and in a workspace of the caller's (npd_last_status)."""
     where = "npd_linear_bwd"
     dev = _device_of(dy, where)
     if dy.dim() != 2 or weight is None or weight.dim() != 2:
@@ -811,7 +828,8 @@ class CEStep:
 
 def npd_cross_entropy(hidden, weight, labels, *, grads=True, stream=None, **kw):
     """One cross-entropy step with new results: (nll, lse, d_hidden, d_weight), the gradients None without
-    `grads`.  Further arguments as for CEStep, which a loop over fixed buffers uses instead."""
+    `grads`.  Further arguments as for CEStep, which a loop over fixed buffers uses instead.  A wait that ran out on
+    the device shows in npd_device_status."""
     if not grads:
         kw["d_hidden"] = kw["d_weight"] = None
     s = CEStep(hidden, weight, labels, stream=stream, **kw)

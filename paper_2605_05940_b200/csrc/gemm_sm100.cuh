@@ -604,7 +604,7 @@ gemm_bf16_kernel(const __grid_constant__ CUtensorMap tmap_a0, const __grid_const
   cluster_sync_all();
   tc_fence_after_sync();
   if (warp == 1) tmem_dealloc_pair(tmem_base, TMEM_COLS);
-  if (threadIdx.x == 0 && *abort_flag != 0 && p.status != nullptr) atomicCAS(p.status, 0, kStatusTimeout);
+  if (threadIdx.x == 0 && *abort_flag != 0) report_timeout(p.status);
 }
 
 }  // namespace npd

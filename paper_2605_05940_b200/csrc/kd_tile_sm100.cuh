@@ -640,7 +640,7 @@ kd_tile_kernel(const __grid_constant__ CUtensorMap tmap_h, const __grid_constant
     __syncwarp();
     tmem_dealloc_pair(tmem_base, TMEM_COLS);
   }
-  if (threadIdx.x == 0 && *abort_flag != 0 && p.status != nullptr) atomicCAS(p.status, 0, kStatusTimeout);
+  if (threadIdx.x == 0 && *abort_flag != 0) report_timeout(p.status);
 }
 
 }  // namespace npd

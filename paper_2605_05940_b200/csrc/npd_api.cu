@@ -866,6 +866,23 @@ int npd_last_status(const void* workspace, void* cuda_stream, int32_t* host_stat
   return cudaStreamSynchronize(st) == cudaSuccess ? NPD_OK : NPD_ECUDA;
 }
 
+int npd_device_status(void* cuda_stream, int32_t* host_status) {
+  if (host_status == nullptr) return NPD_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  int32_t word = 0;
+  if (cudaMemcpyFromSymbolAsync(&word, g_device_status, sizeof(word), 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess)
+    return NPD_ECUDA;
+  if (word != 0) {
+    const int32_t none = 0;
+    if (cudaMemcpyToSymbolAsync(g_device_status, &none, sizeof(none), 0, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess)
+      return NPD_ECUDA;
+  }
+  *host_status = word;
+  return NPD_OK;
+}
+
 // ---------------------------------------------------------------------------------------
 // Forward pass for callers that cannot allocate device memory.
 //

@@ -263,7 +263,7 @@ pair_tile_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_consta
     __syncwarp();
     tmem_dealloc_pair(tmem_base, TMEM_COLS);
   }
-  if (threadIdx.x == 0 && *abort_flag != 0 && p.status != nullptr) atomicCAS(p.status, 0, kStatusTimeout);
+  if (threadIdx.x == 0 && *abort_flag != 0) report_timeout(p.status);
 }
 
 }  // namespace npd

@@ -17,6 +17,16 @@ constexpr int kStatusTimeout = -8;
 // Upper bound of any device-side wait, in SM clock cycles (about 2 s).
 constexpr long long kWaitLimitCycles = 4000000000LL;
 
+// Of this device: kStatusTimeout once a kernel's bounded wait has run out, until npd_device_status reads it.  A
+// kernel whose caller gave no status word, or has let go of it, still leaves a trace here.
+static __device__ int g_device_status;
+
+// What a kernel does (one thread) after a wait of its own has run out.  `status`: its call's word, or NULL.
+__device__ __forceinline__ void report_timeout(int* status) {
+  if (status != nullptr) atomicCAS(status, 0, kStatusTimeout);
+  atomicExch(&g_device_status, kStatusTimeout);
+}
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) {
   return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }

@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(128) wait_timeout_selftest_kernel(long long li
   const bool ok = named_barrier_vote(1, 128, okw);
   const int none_ok = __syncthreads_and(okw ? 0 : 1);
   if (threadIdx.x == 0) {
-    if (!ok && abort_flag != 0) atomicCAS(out, 0, kStatusTimeout);
+    if (!ok && abort_flag != 0) report_timeout(out);
     out[1] = none_ok;
     out[2] = static_cast<int>(dt & 0x7fffffff);
   }
