@@ -490,7 +490,7 @@ int npd_ce_fwd_bwd(const npd_ce_args* args, void* cuda_stream);
 enum {
   NPD_ACT_NONE = 0,
   NPD_ACT_RELU = 1,
-  NPD_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function */
+  NPD_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution function; in fp32 off by (2 z^2 + 32) 2^-24 of the value */
   NPD_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
   NPD_ACT_SILU = 4       /* z / (1 + e^-z) */
 };

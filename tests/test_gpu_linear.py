@@ -244,3 +244,30 @@ def test_accumulation_into_a_new_dw_starts_at_zero():
     _, dw, _ = B.npd_linear_bwd(dy, x, w, want_dx=False, dw_dtype=torch.float32, accumulate_dw=True)
     _, plain, _ = B.npd_linear_bwd(dy, x, w, want_dx=False, dw_dtype=torch.float32)
     assert torch.equal(dw, plain)                         # one add to zero per element
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_gelu_is_right_relative_to_itself_far_out(rows):
+    # z Phi(z) and its slope from z = -12.5 on, where Phi(z) is about 4e-36 and still a normal number.  Tolerance, relative to
+    # the value: e^(-z^2/2) has an argument with three roundings, so z^2/2 * 3 u <= 1.5 z^2 u (2 z^2 u with the exponential's
+    # own), 4 u more from the exponential instruction; the factor t P(t) beside it a fit of 1e-7 (1.7 u), the coefficients'
+    # roundings (1.8 u) and the multiply-adds' (their partial sums add up to 3 P(t): 3 u), t from a denominator with two
+    # roundings and a reciprocal good to 2 units (6 u, on which t P(t) depends with a power of at most 2.62: 15.7 u), three
+    # products (3 u): 29.2 u, below 32 u.  u = 2^-24.
+    v = torch.cat([torch.linspace(-12.5, -0.5, 97, device=DEV), torch.tensor([-12.25, -8.0, -6.0, -5.0, -4.0, -0.25, -1e-3], device=DEV)]).to(BF16)
+    x = torch.zeros((rows, 8), device=DEV, dtype=BF16)
+    x[:, 0] = 1
+    w = torch.zeros((v.numel(), 8), device=DEV, dtype=BF16)
+    w[:, 0] = v
+    V = host(v)
+    want, slope = orc.activation(V, "gelu")
+    rel = (32 + 2 * V * V) * u(F32)
+    for dt in (F32, BF16):
+        y, z = B.npd_linear_fwd(x, w, activation=B.NPD_ACT_GELU, y_dtype=dt, want_preact=True)
+        assert torch.equal(z[0], v)
+        assert np.all(np.abs(host(y) - want) <= np.abs(want) * (rel + u(dt) * (1 + rel))), dt
+    _, _, db = B.npd_linear_bwd(torch.ones((1, 104), device=DEV, dtype=BF16), x[:1], w, preact=z[:1], activation=B.NPD_ACT_GELU,
+                                want_dbias=True)
+    # Phi(z) and z phi(z) have opposite signs
+    phi = np.exp(-0.5 * V * V) / np.sqrt(2 * np.pi)
+    assert np.all(np.abs(host(db) - slope) <= rel * (want / V + np.abs(V) * phi) + u(F32) * np.abs(slope))
