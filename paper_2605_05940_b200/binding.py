@@ -698,7 +698,8 @@ class NormJoin:
     afterwards turns their gradient into those of x, residual, gate and gains: dx, dresidual, d_post_weight,
     d_pre_weight, d_gate.  For a step without d_hidden (scoring, a head trained alone) the join is made with
     grads=False; otherwise the step refuses it.  The backward reads x, gate and gains again, so the step's hidden
-    states and d_hidden lie apart from them (hidden may be x's memory with grads=False).  Arguments as for npd_norm_fwd."""
+    states and d_hidden lie apart from them (hidden may be x's memory with grads=False).  The buffers belong to one
+    run at a time.  Arguments as for npd_norm_fwd."""
 
     def __init__(self, x, residual=None, *, grads=True, **how):
         self.x, self.residual, self.how, self.grads = x, residual, how, grads
@@ -844,6 +845,9 @@ class KDStep:
     def __init__(self, batch, *, grads=True, dw_dtype=torch.bfloat16, grad_chunk_cols=0, grad_scale=None,
                  kd_lambda=None, topk_values=None, topk_indices=None, flags=0, norm=None):
         self.norm = norm   # a NormJoin that writes batch.hidden before, and takes d_hidden back after the step
+        # the tensors whose addresses the step keeps, whatever the batch holds later
+        self._inputs = (batch.hidden, batch.weight, batch.teacher if topk_values is None else None, batch.cu_seqlens,
+                        batch.loss_mask, batch.labels)
         dev = batch.hidden.device
         T, d, V = batch.T, batch.d, batch.V
         f32 = dict(dtype=torch.float32, device=dev)
@@ -880,7 +884,7 @@ class KDStep:
 
     def _run(self, args, stream):
         if self.norm is not None:
-            self.norm.forward(self.batch.hidden, stream)
+            self.norm.forward(self._inputs[0], stream)
         npd_kd_fwd_bwd(args, stream)
         if self.norm is not None and self.norm.grads:
             self.norm.backward(self.d_hidden, stream)

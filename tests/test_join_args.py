@@ -95,3 +95,16 @@ def test_touch_knows_the_rows_of_a_window():
     assert not B._touch(base[:, :8], base[:, 8:16]) and not B._touch(base[:, 16:], base[1:, :16])
     assert B._touch(base[:, :9], base[:, 8:16]) and B._touch(base[:, 16:], base[:, 15:17])
     assert not B._touch(base, torch.zeros((8, 32))) and not B._touch(base, None) and B._touch(base[0], base[:1])
+
+
+def test_the_join_writes_the_hidden_states_that_the_step_reads(calls, monkeypatch):
+    # a batch object may be given other tensors later on; a step stays with those it was made for
+    hidden, weight = _mat(), _mat(V)
+    batch = types.SimpleNamespace(T=T, d=D, V=V, hidden=hidden, weight=weight, teacher=_mat(T, V), tau=1.0, n_loss=T,
+                                  cu_seqlens=None, loss_mask=None, labels=None)
+    step = B.KDStep(batch, norm=B.NormJoin(_mat(), _mat(), pre_weight=torch.ones(D)))
+    batch.hidden = _mat()
+    written = []
+    monkeypatch.setattr(B, "npd_norm_fwd", lambda x, r, y, **kw: written.append(y.data_ptr()))
+    step.run()
+    assert written == [step.args.hidden] == [hidden.data_ptr()]
