@@ -273,7 +273,9 @@ struct CeForwardEpi {
 // them, and take longer than reading the weights (T = 1: 157 us at d = 1536 and 300 us at d = 4096, V = 151,936).  A
 // block takes 16 vocabulary rows at a time (rows_sm100.cuh), one group after the other across the whole grid;
 // every (token, row of 16) has a thread that keeps a running maximum and sum of the logits it sees.  They are merged
-// over the block at its end, and over the blocks by ce_merge_kernel.  Beyond 8 tokens the tiles are as fast.
+// over the block at its end, and over the blocks by ce_merge_kernel.  The instruction holds 8 tokens; from 9 on the tiles
+// take over, which are slower at first (the whole forward at V = 151,936: T = 8 85 us at d = 1536 and 203 at d = 4096, T = 9 112 and
+// 284, T = 32 118 and 256, T = 64 104 at d = 1536).
 struct CeRowsParams {
   int V, d;
   const int* plan;

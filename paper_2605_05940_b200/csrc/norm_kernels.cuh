@@ -511,7 +511,9 @@ __global__ void __launch_bounds__(kThreads, kVec == 1 ? 1024 / kThreads : 1) nor
 // is a multiple of 8 besides (no vector is partly outside the row); 3: of 256 (no thread is; d = 2048, T = 40,000: 160 us,
 // as form 2 172 us, as form 1 170; an fp32 stream as form 1 296 us instead of 228).  kVec > 1: 2 or 0 (d = 8192, T =
 // 10,000: 234 us as form 2, 254 as form 0; d = 12,288, T = 6664: 434 and 572 us).  A call with a missing part takes
-// form 0, which tests for it (a per-token gate at d = 1536, T = 53,328: 372 us in form 0, 202 us in its own).
+// form 0, which tests for it and has nothing in flight ahead (a per-token gate at d = 1536, T = 53,328: 372 us in form 0, 202 us
+// in its own; the norm in front of an LM head, where no gradient arrives at h from elsewhere, T = 8192, bf16: d = 1536
+// 52 us, d = 4096 129 us, 37 and 40 % of the copy rate).
 // kNarrow: see norm_cfg (d = 128, T = 65,536, bf16: 23 us; a block of one warp per row took 41 us).
 template <bool kF32, int kVec, int kForm, bool kGate, int kThreads, bool kNarrow>
 __global__ void __launch_bounds__(kThreads, 512 / kThreads) norm_bwd_kernel(const NormParams p) {
