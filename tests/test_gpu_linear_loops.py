@@ -69,7 +69,7 @@ def _check_backward(dy, x, w, z, act, got):
         _inside(db, dz.sum(0), u(F32) * (M / 8 + 64) * dz.abs().sum(0) + edz.sum(0), "dbias")
 
 
-# at 74 CTA pairs 64 x 256 tiles of the first, 128 wide ones of the second and third, 256 wide ones of the others
+# with 74 CTA pairs the first takes tiles 64 columns wide, the second and third 128, the others 256
 @pytest.mark.parametrize("M,N,K", [(300, 1500, 520), (500, 3000, 200), (129, 9001, 72), (1000, 9000, 72), (4100, 2300, 136),
                                    (4097, 2315, 65)])
 @pytest.mark.parametrize("yd", [BF16, F32])
@@ -99,8 +99,8 @@ def test_many_rows_per_warp_of_the_slopes(M, N, K, act):
     assert torch.equal(alone[2], got[2])
 
 
-# more than 74 tiles of 256 x 512 in both products, the longer contraction first in either; the last one deals the short
-# tiles to some pairs only
+# tiles of 256 x 512 for more than one round of the 74 CTA pairs, the longer contraction in dw or in dx; some pairs take one
+# more of the long tiles and fewer of the short ones (the last case: 24 long tiles, 632 short ones)
 @pytest.mark.parametrize("M,N,K", [(6000, 5000, 2056), (5001, 6003, 2500), (9000, 2100, 5000), (2100, 9000, 5000), (20000, 600, 4000)])
 @pytest.mark.parametrize("act", ["none", "silu"])
 def test_more_tiles_than_pairs_in_the_backward(M, N, K, act):
